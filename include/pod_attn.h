@@ -296,6 +296,102 @@ pod_status pod_attn_forward_static(const void *prefill_q, const void *decode_q,
                                    void *out, const pod_attn_plan *plan, int32_t mode, void *stream);
 
 /*
+ * What a batch needs before its attention: blocks and slots for the new tokens, and their keys and values in the cache.
+ * Both calls take the pod_attn_params of the batch (validated as the plan does; fields about cutting work are not
+ * looked at), launch one kernel on `stream`, keep no state, allocate nothing and may be recorded into a graph.
+ *
+ * A slot names a token's place in the cache: for a paged cache block * block_size + offset, for a contiguous one
+ * cache_row * max_len + token with max_len = kv_seq_stride / (n_kv_heads * head_dim).  Rows are the rows of `out` of the
+ * attention call: prefill rows first, then a row per decode request; rows behind them are padding (a batch padded to the
+ * size of a captured graph).
+ */
+
+/*
+ * Blocks, slots and positions of a batch's new tokens, from the request lengths on the device.
+ *
+ * Request r holds ceil((kv_len - q_len) / block_size) blocks and needs ceil(kv_len / block_size).  The blocks it lacks are
+ * taken from `free_blocks` in request order, lowest index first, and entered in its row of block_table; the other entries
+ * are left as they are.
+ *   seq_meta     device, int32 [n_prefill + n_decode][4] as for pod_attn_forward; read when the kernel runs
+ *   free_blocks  device, int32 [n_free]; NULL for a contiguous cache (then n_free = 0)
+ *   block_table  device, int32 [n_cache_rows][max_blocks_per_seq], read and written; NULL for a contiguous cache
+ *   slots,       device, int32 [n_rows] each: slot and position of every row.  n_rows is at least the batch's rows; padding
+ *   positions    rows get slot -1 and position 0.  A row that is no row of `out` because prefill rows leave a gap, or decode
+ *                rows a q_start out, is not written.
+ *   report       device, int32 [4]: blocks taken, blocks missing, requests refused, rows of the batch
+ * With fewer free blocks than the batch needs nothing is taken: block_table is left as it is, every slot is -1 and report
+ * says how many blocks are missing.  A request that cannot be (q_len < 1, kv_len < q_len, a decode with q_len other than
+ * 1, cache_row outside the cache, kv_len beyond its row, q_start outside the rows) takes no blocks, and those of its rows
+ * that exist get slot -1 and position 0.  A row whose token lies in a block entry outside [0, n_blocks) gets slot -1 as well.
+ * Requests that share a cache_row must not need blocks for it, and a free list must not name a block twice.
+ */
+pod_status pod_attn_build_tables(const pod_attn_params *params, const int32_t *seq_meta, const int32_t *free_blocks,
+                                 int32_t n_free, int32_t *block_table, int32_t n_rows, int32_t *slots, int32_t *positions,
+                                 int32_t *report, void *stream);
+
+/* Which channels form a pair that is rotated together. */
+typedef enum {
+    POD_ROPE_HALF = 0,          /* i and i + rot_dim / 2                                          */
+    POD_ROPE_INTERLEAVED = 1    /* 2 i and 2 i + 1                                                */
+} pod_rope_layout;
+
+/* How the frequencies f_i = theta^(-2 i / rot_dim) (radians per position) are stretched for long contexts.  With keep = 1 a
+ * frequency stays, with keep = 0 it is divided by `factor`, in between it is keep * f + (1 - keep) * f / factor. */
+typedef enum {
+    POD_ROPE_PLAIN = 0,         /* keep = 1                                                       */
+    POD_ROPE_LINEAR = 1,        /* keep = 0                                                       */
+    POD_ROPE_BY_PARTS = 2,      /* keep rises linearly from 0 to 1 with the turns that the pair makes over trained_len
+                                   positions, from `low` to `high` of them                        */
+    POD_ROPE_BY_INDEX = 3       /* keep falls linearly from 1 to 0 with the pair's index, from floor(index(high)) to
+                                   ceil(index(low)), index(t) = rot_dim ln(trained_len / (2 pi t)) / (2 ln theta), both
+                                   held to [0, rot_dim - 1] and at least 0.001 apart                */
+} pod_rope_scaling;
+
+typedef struct {
+    int32_t layout;             /* pod_rope_layout                                                */
+    int32_t scaling;            /* pod_rope_scaling                                               */
+    int32_t rot_dim;            /* the first rot_dim channels are rotated: a multiple of 16, at most head_dim */
+    float   cos_sin_scale;      /* multiplies cosine and sine (1 in normal use)                   */
+    double  theta;              /* > 1                                                            */
+    double  factor;             /* > 0; read with a scaling other than POD_ROPE_PLAIN             */
+    double  trained_len, low, high;  /* > 0, low < high; read with POD_ROPE_BY_PARTS and POD_ROPE_BY_INDEX */
+} pod_rope_params;
+
+/* The frequencies as the kernels read them, worked out in 64 bits on the host: table[i] (i < rot_dim / 2) is pair i's
+ * turns per position modulo 1, times 2^64.  A position times that, modulo 2^64, is the pair's angle, with no loss for
+ * any position.  The caller copies the table to the device. */
+pod_status pod_attn_rope_table(const pod_rope_params *rope, uint64_t *table);
+
+/* RMS normalisation of each head: x * 1 / sqrt(mean of x^2 over head_dim + eps) * (weight + weight_offset). */
+typedef struct {
+    const void *q_weight;       /* device, [head_dim] in the 16-bit type, or NULL: weight 1, no offset */
+    const void *k_weight;
+    float   eps;                /* >= 0                                                           */
+    float   weight_offset;      /* 0, or 1 where weights are stored as what they add to 1        */
+    int32_t normalise_q, normalise_k;   /* 0: those heads are not normalised                       */
+} pod_head_norm;
+
+/*
+ * The projections of the batch's new tokens, normalised, rotated and put where the attention call reads them.
+ * Query and key heads: normalisation (if any), then rotation (if any) by their row's position; query heads go to q_out,
+ * key heads and the value heads as they are into the cache at the row's slot.  All arithmetic is fp32, rounded once.
+ *   q, k, v      device, 16-bit: row i's heads lie head after head from q + i * q_stride (elements; multiples of 8, so that a
+ *                projection of all three is passed as three pointers with one stride)
+ *   rope         host, or NULL: no rotation;  rope_table device, the table above for `rope`
+ *   norm         host, or NULL: no normalisation
+ *   slots,       device, int32 [n_rows], as pod_attn_build_tables leaves them.  A row with a negative slot, or one beyond
+ *   positions    the cache, is padding: nothing of it is read or written.  Rows must not share a slot.
+ *   q_out        device, [n_rows][Hq][d]: prefill_q, and behind the prefill rows decode_q, of the attention call.  May be
+ *                q itself where q_stride is Hq * d; must not overlap the inputs otherwise
+ *   k_cache, v_cache  the cache of `params`
+ * Pointers to 16-bit data and the table must be 16-byte aligned.  n_rows may be 0.
+ */
+pod_status pod_attn_append(const pod_attn_params *params, const pod_rope_params *rope, const uint64_t *rope_table,
+                           const pod_head_norm *norm, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride, const int32_t *slots, const int32_t *positions, int32_t n_rows,
+                           void *q_out, void *k_cache, void *v_cache, void *stream);
+
+/*
  * The role rule of the on-device binder (Section 4.1, the scheduling listing), host-callable for
  * tests: the first operation of the workgroup that holds `ticket` (arrivals on its hardware unit
  * before it, counted from 0) on unit `unit`: 0 prefill when (ticket + 2 * unit) mod (p + d) < p,

@@ -15,6 +15,7 @@
 #include "pod_common.h"
 #include "pod_launch.h"
 #include "pod_planner.h"
+#include "pod_tokens.h"
 
 struct pod_attn_plan {
     pod::Plan p;
@@ -581,6 +582,181 @@ pod_status pod_attn_forward_static(const void *prefill_q, const void *decode_q, 
 }
 
 static_assert(pod::kStaticScratchBytes == POD_ATTN_STATIC_SCRATCH_BYTES, "the header states the size of the static scratch");
+
+// Slots of a cache, and how one names a place: its block (or cache row) is the slot divided by per_block.
+static pod_status cache_slots(const pod_attn_params &prm, int32_t *per_block, int32_t *n_slots)
+{
+    const int64_t token_elems = (int64_t)prm.n_kv_heads * prm.head_dim;
+    const int64_t per = prm.block_size > 0 ? prm.block_size : prm.kv_seq_stride / token_elems;
+    const int64_t n = per * (prm.block_size > 0 ? prm.n_blocks : prm.n_cache_rows);
+    if (per < 1) return fail(POD_ERR_INVALID_ARG, "kv_seq_stride holds no token");
+    if (per > INT32_MAX || n > INT32_MAX) return fail(POD_ERR_UNSUPPORTED, "the cache has more than 2^31 - 1 slots");
+    *per_block = (int32_t)per;
+    *n_slots = (int32_t)n;
+    return POD_OK;
+}
+
+pod_status pod_attn_build_tables(const pod_attn_params *params, const int32_t *seq_meta, const int32_t *free_blocks,
+                                 int32_t n_free, int32_t *block_table, int32_t n_rows, int32_t *slots, int32_t *positions,
+                                 int32_t *report, void *stream)
+{
+    if (!params) return fail(POD_ERR_INVALID_ARG, "params is null");
+    const pod_attn_params &prm = *params;
+    std::string err;
+    const pod_status checked = pod::check_params(prm, err);
+    if (checked != POD_OK) return fail(checked, err);
+    const bool paged = prm.block_size > 0;
+    const int64_t n_req = (int64_t)prm.n_prefill + prm.n_decode;
+    if (n_req > INT32_MAX / 4) return fail(POD_ERR_UNSUPPORTED, "too many requests");
+    if (n_rows < 0 || n_free < 0) return fail(POD_ERR_INVALID_ARG, "negative n_rows or n_free");
+    if (n_rows < prm.n_decode) return fail(POD_ERR_INVALID_ARG, "n_rows does not hold the decode rows");
+    if (!report || (n_rows > 0 && (!slots || !positions))) return fail(POD_ERR_INVALID_ARG, "slots, positions or report is null");
+    if (n_req > 0 && !seq_meta) return fail(POD_ERR_INVALID_ARG, "seq_meta is null");
+    if (paged && n_req > 0 && !block_table) return fail(POD_ERR_INVALID_ARG, "block_table is null for a paged cache");
+    if (paged ? n_free > 0 && !free_blocks : n_free != 0)
+        return fail(POD_ERR_INVALID_ARG, paged ? "free_blocks is null" : "a contiguous cache has no free blocks");
+    if ((((uintptr_t)seq_meta | (uintptr_t)free_blocks | (uintptr_t)block_table | (uintptr_t)slots | (uintptr_t)positions |
+          (uintptr_t)report) & 3u) != 0)
+        return fail(POD_ERR_INVALID_ARG, "the 32-bit arrays must be 4-byte aligned");
+    pod::TableArgs a;
+    std::memset(&a, 0, sizeof a);
+    int32_t per_block = 0, n_slots = 0;
+    const pod_status slotted = cache_slots(prm, &per_block, &n_slots);
+    if (slotted != POD_OK) return slotted;
+    a.seq_meta = seq_meta; a.free_blocks = free_blocks; a.block_table = block_table;
+    a.slots = slots; a.positions = positions; a.report = report;
+    a.n_free = n_free; a.n_prefill = prm.n_prefill; a.n_decode = prm.n_decode; a.n_rows = n_rows;
+    a.block_size = prm.block_size;
+    a.per_row = paged ? (int32_t)std::min<int64_t>((int64_t)prm.max_blocks_per_seq * prm.block_size, INT32_MAX) : per_block;
+    a.magic = pod::division_magic(per_block);
+    a.max_blocks = prm.max_blocks_per_seq; a.n_cache_rows = prm.n_cache_rows; a.n_blocks = prm.n_blocks;
+    a.n_decode_wgs = (prm.n_decode + pod::kWgThreads - 1) / pod::kWgThreads;
+    if (prm.n_prefill > 0) {
+        const int64_t chunks = ((int64_t)n_rows - prm.n_decode + pod::kWgThreads - 1) / pod::kWgThreads;
+        a.wgs_per_prefill = (int32_t)std::min<int64_t>(64, std::max<int64_t>(1, (chunks + prm.n_prefill - 1) / prm.n_prefill));
+    } else {
+        a.n_decode_wgs = std::max(a.n_decode_wgs, 1);        // the report, and rows of an empty batch
+    }
+    const hipError_t e = pod::launch_tables(a, (hipStream_t)stream);
+    return e == hipSuccess ? POD_OK : fail_hip(e, "launching the table kernel");
+}
+
+// What both users of the frequencies check.
+static pod_status check_rope(const pod_rope_params &r)
+{
+    if (r.layout != POD_ROPE_HALF && r.layout != POD_ROPE_INTERLEAVED) return fail(POD_ERR_INVALID_ARG, "unknown rope layout");
+    if (r.scaling < POD_ROPE_PLAIN || r.scaling > POD_ROPE_BY_INDEX) return fail(POD_ERR_INVALID_ARG, "unknown rope scaling");
+    if (r.rot_dim <= 0 || r.rot_dim > 256) return fail(POD_ERR_INVALID_ARG, "rot_dim must be positive and at most head_dim");
+    if (r.rot_dim % 16 != 0) return fail(POD_ERR_UNSUPPORTED, "rot_dim must be a multiple of 16");
+    if (!(r.theta > 1.0) || !std::isfinite(r.theta)) return fail(POD_ERR_INVALID_ARG, "theta must be above 1 and finite");
+    if (!std::isfinite(r.cos_sin_scale)) return fail(POD_ERR_INVALID_ARG, "cos_sin_scale must be finite");
+    if (r.scaling != POD_ROPE_PLAIN && (!(r.factor > 0.0) || !std::isfinite(r.factor)))
+        return fail(POD_ERR_INVALID_ARG, "factor must be positive and finite");
+    if (r.scaling >= POD_ROPE_BY_PARTS &&
+        (!(r.trained_len > 0.0) || !std::isfinite(r.trained_len) || !(r.low > 0.0) || !(r.high > r.low) || !std::isfinite(r.high)))
+        return fail(POD_ERR_INVALID_ARG, "trained_len must be positive and 0 < low < high");
+    return POD_OK;
+}
+
+pod_status pod_attn_rope_table(const pod_rope_params *rope, uint64_t *table)
+{
+    if (!rope || !table) return fail(POD_ERR_INVALID_ARG, "rope or table is null");
+    const pod_status checked = check_rope(*rope);
+    if (checked != POD_OK) return checked;
+    const double pi2 = 6.283185307179586476925286766559;
+    const int n = rope->rot_dim / 2;
+    double from = 0.0, to = 0.0;                             // pair indices between which keep falls, POD_ROPE_BY_INDEX
+    if (rope->scaling == POD_ROPE_BY_INDEX) {
+        auto index = [&](double t) { return rope->rot_dim * std::log(rope->trained_len / (t * pi2)) / (2.0 * std::log(rope->theta)); };
+        const double last = rope->rot_dim - 1.0;
+        from = std::min(std::max(std::floor(index(rope->high)), 0.0), last);
+        to = std::min(std::max(std::ceil(index(rope->low)), 0.0), last);
+        to = std::max(to, from + 0.001);
+    }
+    for (int i = 0; i < n; ++i) {
+        const double f = std::pow(rope->theta, -2.0 * i / rope->rot_dim);
+        double keep = 1.0;
+        switch (rope->scaling) {
+        case POD_ROPE_LINEAR: keep = 0.0; break;
+        case POD_ROPE_BY_PARTS: keep = (rope->trained_len * f / pi2 - rope->low) / (rope->high - rope->low); break;
+        case POD_ROPE_BY_INDEX: keep = 1.0 - (i - from) / (to - from); break;
+        default: break;
+        }
+        keep = std::min(std::max(keep, 0.0), 1.0);
+        const double radians = rope->scaling == POD_ROPE_PLAIN ? f : f * keep + f / rope->factor * (1.0 - keep);
+        double turns = radians / pi2;
+        turns -= std::floor(turns);                          // in [0, 1); rounding can make the product 2^64, a full turn
+        const double scaled = turns * 18446744073709551616.0;
+        table[i] = scaled < 18446744073709551616.0 ? (uint64_t)scaled : 0u;
+    }
+    return POD_OK;
+}
+
+pod_status pod_attn_append(const pod_attn_params *params, const pod_rope_params *rope, const uint64_t *rope_table,
+                           const pod_head_norm *norm, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride, const int32_t *slots, const int32_t *positions, int32_t n_rows,
+                           void *q_out, void *k_cache, void *v_cache, void *stream)
+{
+    if (!params) return fail(POD_ERR_INVALID_ARG, "params is null");
+    const pod_attn_params &prm = *params;
+    std::string err;
+    const pod_status checked = pod::check_params(prm, err);
+    if (checked != POD_OK) return fail(checked, err);
+    pod::AppendArgs a;
+    std::memset(&a, 0, sizeof a);
+    int layout = POD_ROPE_HALF;
+    if (rope) {
+        const pod_status st = check_rope(*rope);
+        if (st != POD_OK) return st;
+        if (rope->rot_dim > prm.head_dim) return fail(POD_ERR_INVALID_ARG, "rot_dim must be positive and at most head_dim");
+        if (!rope_table) return fail(POD_ERR_INVALID_ARG, "rope_table is null");
+        layout = rope->layout;
+        a.rot_dim = rope->rot_dim;
+        a.cos_sin_scale = rope->cos_sin_scale;
+        a.table = rope_table;
+    }
+    if (norm && (norm->normalise_q || norm->normalise_k)) {
+        if (!(norm->eps >= 0.f) || !std::isfinite(norm->eps) || !std::isfinite(norm->weight_offset))
+            return fail(POD_ERR_INVALID_ARG, "eps must be finite and not negative, weight_offset finite");
+        a.norm_q = norm->normalise_q != 0;
+        a.norm_k = norm->normalise_k != 0;
+        a.q_weight = norm->q_weight;
+        a.k_weight = norm->k_weight;
+        a.eps = norm->eps;
+        a.weight_offset = norm->weight_offset;
+    }
+    if (n_rows < 0) return fail(POD_ERR_INVALID_ARG, "negative n_rows");
+    if (n_rows == 0) return POD_OK;
+    if (!q || !k || !v || !slots || !positions || !q_out || !k_cache || !v_cache)
+        return fail(POD_ERR_INVALID_ARG, "q, k, v, slots, positions, q_out, k_cache or v_cache is null");
+    const int64_t q_row = (int64_t)prm.n_q_heads * prm.head_dim, kv_row = (int64_t)prm.n_kv_heads * prm.head_dim;
+    if (q_stride < q_row || k_stride < kv_row || v_stride < kv_row) return fail(POD_ERR_INVALID_ARG, "a row stride is shorter than a row");
+    if (((q_stride | k_stride | v_stride) & 7) != 0) return fail(POD_ERR_INVALID_ARG, "row strides must be multiples of 8 elements (rows are read in 16-byte pieces)");
+    if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out | (uintptr_t)k_cache | (uintptr_t)v_cache |
+          (uintptr_t)a.table | (uintptr_t)a.q_weight | (uintptr_t)a.k_weight) & 15u) != 0)
+        return fail(POD_ERR_INVALID_ARG, "q, k, v, q_out, the caches, norm weights and rope_table must be 16-byte aligned");
+    if ((((uintptr_t)slots | (uintptr_t)positions) & 3u) != 0) return fail(POD_ERR_INVALID_ARG, "slots and positions must be 4-byte aligned");
+    if (q_out == q && q_stride != q_row) return fail(POD_ERR_INVALID_ARG, "q_out is q, but q_stride is not n_q_heads * head_dim");
+    const pod_status slotted = cache_slots(prm, &a.per_block, &a.n_slots);
+    if (slotted != POD_OK) return slotted;
+    a.magic = pod::division_magic(a.per_block);
+    a.q = q; a.k = k; a.v = v;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.slots = slots; a.positions = positions;
+    a.q_out = q_out; a.k_cache = k_cache; a.v_cache = v_cache;
+    const int64_t d = prm.head_dim, hkv = prm.n_kv_heads;
+    const bool paged = prm.block_size > 0, head_major = prm.kv_order == POD_KV_HEAD_MAJOR;
+    a.block_elems = paged ? prm.block_size * hkv * d : prm.kv_seq_stride;
+    a.tok_stride = (int32_t)(head_major ? d : hkv * d);
+    a.head_stride = head_major ? (int64_t)a.per_block * d : d;
+    a.n_rows = n_rows; a.n_q_heads = prm.n_q_heads; a.n_kv_heads = prm.n_kv_heads;
+    const int heads = pod::append_heads(prm.head_dim);
+    const int n_steps = (prm.n_q_heads + 2 * prm.n_kv_heads + heads - 1) / heads;
+    a.steps_per_wave = n_steps;
+    const int parts = (n_steps + a.steps_per_wave - 1) / a.steps_per_wave;
+    const hipError_t e = pod::launch_append(a, prm.dtype, prm.head_dim, layout, parts, (hipStream_t)stream);
+    return e == hipSuccess ? POD_OK : fail_hip(e, "launching the append kernel");
+}
 
 int32_t pod_attn_role_for_ticket(int32_t ticket, int32_t prefill_ratio, int32_t decode_ratio, int32_t unit)
 {

@@ -129,10 +129,8 @@ void role_ratio(int policy, int n_prefill_wgs, int n_decode_wgs, int &p, int &d)
     d = std::max(d, 1);
 }
 
-pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n_cus, Plan &plan,
-                      std::string &err)
+pod_status check_params(const pod_attn_params &prm, std::string &err)
 {
-    // ---- parameters --------------------------------------------------------------------
     if (prm.n_prefill < 0 || prm.n_decode < 0) { err = "negative request count"; return POD_ERR_INVALID_ARG; }
     if (prm.n_q_heads <= 0 || prm.n_kv_heads <= 0 || prm.n_q_heads % prm.n_kv_heads != 0) {
         err = "n_q_heads must be a positive multiple of n_kv_heads";
@@ -166,6 +164,16 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         err = "negative tuning parameter";
         return POD_ERR_INVALID_ARG;
     }
+    return POD_OK;
+}
+
+pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n_cus, Plan &plan,
+                      std::string &err)
+{
+    const pod_status checked = check_params(prm, err);
+    if (checked != POD_OK) return checked;
+    const int group = prm.n_q_heads / prm.n_kv_heads;
+    const bool paged = prm.block_size > 0;
     const int n_req = prm.n_prefill + prm.n_decode;
     if (n_req > 0 && seq_meta == nullptr) { err = "seq_meta is null"; return POD_ERR_INVALID_ARG; }
     if (n_cus <= 0) { err = "n_compute_units must be positive"; return POD_ERR_INVALID_ARG; }

@@ -58,6 +58,8 @@ struct Plan {
     size_t evlog_bytes = 0;
 };
 
+// The checks of parameters that every entry point shares.
+pod_status check_params(const pod_attn_params &prm, std::string &err);
 // Validates and fills `plan`; returns POD_OK or an error code with a message in `err`.
 pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n_cus, Plan &plan,
                       std::string &err);

@@ -1,0 +1,274 @@
+// gfx950 kernels for a batch's new tokens: slots and blocks from request lengths, and the append of their projections.
+#include <hip/hip_runtime.h>
+
+#include "pod_tokens.h"
+
+namespace pod {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int32_t i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+#define POD_CONST __attribute__((address_space(4)))
+
+// Quotient and remainder of a non-negative 31-bit number by the divisor whose magic this is.
+__device__ __forceinline__ int divide(int t, int divisor, uint32_t magic, int &rest)
+{
+    if (magic == 0u) { rest = 0; return t; }
+    int q = (int)(((uint64_t)(uint32_t)t * magic) >> 32);
+    rest = t - q * divisor;
+    if (rest < 0) { --q; rest += divisor; }
+    return q;
+}
+
+// ------------------------------------------------------------------------------------------
+// Tables.  One launch and nothing shared between workgroups: each one adds up the blocks of all requests before its own
+// (exclusive prefix sum: request r takes free_blocks[before_r ..]) and of the whole batch (does the list hold enough?)
+// from the request lengths themselves, 16 bytes a request that every workgroup finds in its L2, and then writes its own
+// rows.  What bounds it is the launch and two dependent round trips.  A decode request is a thread; the tokens of a
+// prefill request are dealt to several workgroups.
+// ------------------------------------------------------------------------------------------
+struct Request { int start, q_len, kv_len, row, held, fresh; bool ok; };
+
+__device__ __forceinline__ Request read_request(const TableArgs &a, int r)
+{
+    const i32x4_a4 m = *(const i32x4_a4 *)(a.seq_meta + 4 * (int64_t)r);
+    Request x{m[0], m[1], m[2], m[3], 0, 0, false};
+    const bool decode = r >= a.n_prefill;
+    x.ok = x.q_len >= 1 && x.kv_len >= x.q_len && x.start >= 0 && x.row >= 0 && x.row < a.n_cache_rows && x.kv_len <= a.per_row &&
+           (decode ? x.q_len == 1 && x.start < a.n_decode : x.start <= a.n_rows - x.q_len);
+    if (x.ok && a.block_size > 0) {
+        int rest;
+        x.held = divide(x.kv_len - x.q_len, a.block_size, a.magic, rest);
+        x.held += rest > 0 ? 1 : 0;
+        int need = divide(x.kv_len, a.block_size, a.magic, rest);
+        need += rest > 0 ? 1 : 0;
+        x.fresh = need - x.held;
+    }
+    return x;
+}
+
+__device__ __forceinline__ int64_t wave_sum(int64_t x)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+
+__global__ __launch_bounds__(kWgThreads) void token_tables(TableArgs a)
+{
+    __shared__ int64_t part[kWavesPerWg][4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n_req = a.n_prefill + a.n_decode;
+    const int b = (int)blockIdx.x;
+    const bool decode_wg = b < a.n_decode_wgs;
+    const int prefill_req = decode_wg ? -1 : (b - a.n_decode_wgs) / max(a.wgs_per_prefill, 1);
+    const int first_req = decode_wg ? a.n_prefill + b * kWgThreads : prefill_req;    // the workgroup's (first) request
+    // blocks of the requests before that, of all, prefill rows, refused requests
+    int64_t before = 0, total = 0, prows = 0, refused = 0;
+    for (int r = tid; r < n_req; r += kWgThreads) {
+        const Request x = read_request(a, r);
+        total += x.fresh;
+        before += r < first_req ? x.fresh : 0;
+        prows += r < a.n_prefill ? max(x.q_len, 0) : 0;
+        refused += x.ok ? 0 : 1;
+    }
+    before = wave_sum(before); total = wave_sum(total); prows = wave_sum(prows); refused = wave_sum(refused);
+    if (lane == 0) { part[wave][0] = before; part[wave][1] = total; part[wave][2] = prows; part[wave][3] = refused; }
+    __syncthreads();
+    before = total = prows = refused = 0;
+#pragma unroll
+    for (int w = 0; w < kWavesPerWg; ++w) { before += part[w][0]; total += part[w][1]; prows += part[w][2]; refused += part[w][3]; }
+    const bool enough = total <= a.n_free;
+    const int64_t covered = prows + a.n_decode;
+    if (b == 0 && tid == 0) {
+        a.report[0] = enough ? (int32_t)total : 0;
+        a.report[1] = enough ? 0 : (int32_t)min(total - a.n_free, (int64_t)0x7fffffff);
+        a.report[2] = (int32_t)refused;
+        a.report[3] = (int32_t)min(covered, (int64_t)0x7fffffff);
+    }
+    // padding rows, dealt over the whole launch
+    for (int64_t i = covered + (int64_t)b * kWgThreads + tid; i < a.n_rows; i += (int64_t)gridDim.x * kWgThreads) {
+        a.slots[i] = -1;
+        a.positions[i] = 0;
+    }
+    // Row `at` is token `pos` of request x, whose new blocks are free_blocks[taken ..].
+    auto write_row = [&](const Request &x, int64_t at, int pos, int64_t taken) {
+        if (at < 0 || at >= a.n_rows) return;
+        int slot = -1;
+        if (x.ok && a.block_size == 0) {
+            slot = x.row * a.per_row + pos;
+        } else if (x.ok && enough) {
+            int rest;
+            const int index = divide(pos, a.block_size, a.magic, rest);
+            int32_t *entry = a.block_table + (int64_t)x.row * a.max_blocks + index;
+            int block;
+            if (index >= x.held) {
+                block = a.free_blocks[taken + (index - x.held)];
+                // a new block begins with a new token, whose row enters it
+                if (rest == 0) *entry = block;
+            } else {
+                block = *entry;
+            }
+            if (block >= 0 && block < a.n_blocks) slot = block * a.block_size + rest;
+        }
+        a.slots[at] = slot;
+        a.positions[at] = x.ok ? pos : 0;
+    };
+    if (decode_wg) {
+        const int r = first_req + tid;
+        Request x{};
+        if (r < n_req) x = read_request(a, r);
+        // exclusive prefix sum over the workgroup's requests (a decode takes one block at the most)
+        const uint64_t takes = __ballot(x.fresh > 0);
+        __syncthreads();
+        if (lane == 0) part[wave][0] = __popcll(takes);
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) before += part[w][0];
+        before += __popcll(takes & ((uint64_t(1) << lane) - 1));
+        if (r < n_req && x.start >= 0 && x.start < a.n_decode) write_row(x, prows + x.start, x.kv_len - 1, before);
+    } else {
+        const Request x = read_request(a, prefill_req);
+        const int chunk = (b - a.n_decode_wgs) - prefill_req * a.wgs_per_prefill;
+        const int64_t n = x.start >= 0 ? min((int64_t)x.q_len, (int64_t)a.n_rows - x.start) : 0;
+        for (int64_t i = (int64_t)chunk * kWgThreads + tid; i < n; i += (int64_t)a.wgs_per_prefill * kWgThreads)
+            write_row(x, x.start + i, x.kv_len - x.q_len + (int)i, before);
+    }
+}
+
+hipError_t launch_tables(const TableArgs &a, hipStream_t stream)
+{
+    token_tables<<<dim3(a.n_decode_wgs + a.n_prefill * a.wgs_per_prefill), dim3(kWgThreads), 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------
+// Append.  A lane owns 16 channels of a head as two 16-byte pieces chosen so that both members of every rotated pair are
+// its own: pieces p and p + rot_dim / 16 with the half layout, neighbours with the interleaved one and behind the rotated
+// channels.  Normalising a head is then a sum over head_dim / 16 neighbouring lanes and rotating it needs no exchange.
+// A wavefront works on one row, 1024 / head_dim heads at a time, query, key and value heads alike; a lane's pairs are the
+// same in every head, so that their cosines and sines are worked out once a row.  The angle is a fixed-point product: the
+// pair's turns per position as a fraction of 2^64 times the position, whose upper word is the angle as a signed fraction
+// of a turn to 2^-32, for every position; the sine unit takes turns.
+// ------------------------------------------------------------------------------------------
+template <int DT> struct Elem;
+template <> struct Elem<0> { using t = _Float16; };
+template <> struct Elem<1> { using t = __bf16; };
+
+template <int DT, int D, int ROPE>
+__global__ __launch_bounds__(kWgThreads) void append_tokens(AppendArgs a)
+{
+    using elem = typename Elem<DT>::t;
+    typedef elem e8 __attribute__((ext_vector_type(8)));
+    constexpr int LPH = D / 16, HPW = kWaveSize / LPH;
+    const int lane = threadIdx.x & 63;
+    const int row = (int)blockIdx.x * kWavesPerWg + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row >= a.n_rows) return;
+    const int slot = ((const POD_CONST int32_t *)a.slots)[row], pos = ((const POD_CONST int32_t *)a.positions)[row];
+    if (slot < 0 || slot >= a.n_slots) return;
+    int at;
+    const int block = divide(slot, a.per_block, a.magic, at);
+    const int64_t cache_base = (int64_t)block * a.block_elems + (int64_t)at * a.tok_stride;
+    const int sub = lane % LPH, pairs = a.rot_dim / 16;
+    const bool turns = sub < pairs;
+    int c0 = 2 * sub, c1 = 2 * sub + 1;               // the lane's pieces of a head
+    if (ROPE == POD_ROPE_HALF && turns) { c0 = sub; c1 = sub + pairs; }
+    float cs[8], sn[8];
+    if (turns) {
+        const uint64_t *f = a.table + 8 * sub;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const u32x4 w = *(const u32x4 *)(f + i);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t angle = __umulhi((uint32_t)pos, w[2 * j]) + (uint32_t)pos * w[2 * j + 1];
+                if (pos < 0) angle -= w[2 * j];
+                const float x = (float)(int32_t)angle * 0x1p-32f;
+                cs[i + j] = __builtin_amdgcn_cosf(x) * a.cos_sin_scale;
+                sn[i + j] = __builtin_amdgcn_sinf(x) * a.cos_sin_scale;
+            }
+        }
+    }
+    const int n_heads = a.n_q_heads + 2 * a.n_kv_heads;
+    const int n_steps = (n_heads + HPW - 1) / HPW;
+    const int s0 = (int)blockIdx.y * a.steps_per_wave, s1 = min(n_steps, s0 + a.steps_per_wave);
+    for (int s = s0; s < s1; ++s) {
+        const int head = s * HPW + lane / LPH;
+        if (head >= n_heads) continue;                // (whole groups of lanes; the last step alone)
+        const bool is_q = head < a.n_q_heads, is_k = !is_q && head < a.n_q_heads + a.n_kv_heads;
+        const int kv = head - a.n_q_heads - (is_k ? 0 : a.n_kv_heads);
+        const elem *src = is_q ? (const elem *)a.q + row * a.q_stride + head * D
+                               : (is_k ? (const elem *)a.k + row * a.k_stride : (const elem *)a.v + row * a.v_stride) + kv * D;
+        elem *dst = is_q ? (elem *)a.q_out + ((int64_t)row * a.n_q_heads + head) * D
+                         : (elem *)(is_k ? a.k_cache : a.v_cache) + cache_base + kv * a.head_stride;
+        e8 r0 = *(const e8 *)(src + c0 * 8), r1 = *(const e8 *)(src + c1 * 8);
+        const bool norm = is_q ? a.norm_q : is_k && a.norm_k;
+        float x[8], y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { x[i] = (float)r0[i]; y[i] = (float)r1[i]; }
+        if (a.norm_q | a.norm_k) {
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss += x[i] * x[i] + y[i] * y[i];
+#pragma unroll
+            for (int d = 1; d < LPH; d *= 2) ss += __shfl_xor(ss, d);
+            const float inv = rsqrtf(ss * (1.f / D) + a.eps);
+            if (norm) {
+                const elem *w = (const elem *)(is_q ? a.q_weight : a.k_weight);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] *= inv * (w ? (float)w[c0 * 8 + i] + a.weight_offset : 1.f);
+                    y[i] *= inv * (w ? (float)w[c1 * 8 + i] + a.weight_offset : 1.f);
+                }
+            }
+        }
+        const bool turned = turns && (is_q || is_k);
+        if (turned) {
+            if (ROPE == POD_ROPE_HALF) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float u = x[i], v = y[i];
+                    x[i] = u * cs[i] - v * sn[i];
+                    y[i] = v * cs[i] + u * sn[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float u = x[2 * i], v = x[2 * i + 1];
+                    x[2 * i] = u * cs[i] - v * sn[i];
+                    x[2 * i + 1] = v * cs[i] + u * sn[i];
+                    u = y[2 * i]; v = y[2 * i + 1];
+                    y[2 * i] = u * cs[4 + i] - v * sn[4 + i];
+                    y[2 * i + 1] = v * cs[4 + i] + u * sn[4 + i];
+                }
+            }
+        }
+        if (norm || turned) {                         // other channels are copied as they are
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { r0[i] = (elem)x[i]; r1[i] = (elem)y[i]; }
+        }
+        *(e8 *)(dst + c0 * 8) = r0;
+        *(e8 *)(dst + c1 * 8) = r1;
+    }
+}
+
+template <int DT, int D>
+static hipError_t launch_append_as(const AppendArgs &a, int layout, int parts, hipStream_t stream)
+{
+    const dim3 grid((a.n_rows + kWavesPerWg - 1) / kWavesPerWg, parts), threads(kWgThreads);
+    if (layout == POD_ROPE_HALF) append_tokens<DT, D, POD_ROPE_HALF><<<grid, threads, 0, stream>>>(a);
+    else append_tokens<DT, D, POD_ROPE_INTERLEAVED><<<grid, threads, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, int layout, int parts, hipStream_t stream)
+{
+    if (dtype == POD_F16 && head_dim == 64) return launch_append_as<0, 64>(a, layout, parts, stream);
+    if (dtype == POD_F16 && head_dim == 128) return launch_append_as<0, 128>(a, layout, parts, stream);
+    if (dtype == POD_F16 && head_dim == 256) return launch_append_as<0, 256>(a, layout, parts, stream);
+    if (dtype == POD_BF16 && head_dim == 64) return launch_append_as<1, 64>(a, layout, parts, stream);
+    if (dtype == POD_BF16 && head_dim == 128) return launch_append_as<1, 128>(a, layout, parts, stream);
+    if (dtype == POD_BF16 && head_dim == 256) return launch_append_as<1, 256>(a, layout, parts, stream);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace pod

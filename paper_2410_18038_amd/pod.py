@@ -7,6 +7,7 @@ There is no fallback: if the library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import dataclasses
 import os
 from typing import Optional
 
@@ -33,6 +34,7 @@ KV_TOKEN_MAJOR, KV_HEAD_MAJOR = 0, 1
 EXPORTS = ["pod_attn_plan_create", "pod_attn_plan_destroy", "pod_attn_plan_info_get",
            "pod_attn_workspace_size", "pod_attn_plan_set_trace", "pod_attn_plan_set_event_log",
            "pod_attn_plan_upload", "pod_attn_forward", "pod_attn_forward_static",
+           "pod_attn_build_tables", "pod_attn_rope_table", "pod_attn_append",
            "pod_attn_role_for_ticket", "pod_attn_simulate_launch", "pod_attn_plan_prefill_item", "pod_attn_plan_prefill_item_of_workgroup", "pod_attn_plan_decode_unit",
            "pod_attn_plan_decode_queue",
            "pod_attn_probe_hbm_read", "pod_attn_probe_mfma", "pod_attn_probe_issue", "pod_attn_probe_colocation",
@@ -66,6 +68,17 @@ class PlanInfo(ctypes.Structure):
                 ("n_prefill_rows", ctypes.c_int64), ("n_partial_rows", ctypes.c_int64),
                 ("workspace_bytes", ctypes.c_int64), ("prefill_heavy_advised", ctypes.c_int32),
                 ("prefill_heavy_chosen", ctypes.c_int32)]
+
+
+class RopeParams(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("scaling", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("cos_sin_scale", ctypes.c_float), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("trained_len", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class HeadNormParams(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("weight_offset", ctypes.c_float), ("normalise_q", ctypes.c_int32), ("normalise_k", ctypes.c_int32)]
 
 
 _lib = None
@@ -106,6 +119,14 @@ def lib():
                                        ctypes.c_int32, vp]
         L.pod_attn_forward_static.restype = ctypes.c_int
         L.pod_attn_forward_static.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int32, vp]
+        L.pod_attn_build_tables.restype = ctypes.c_int
+        L.pod_attn_build_tables.argtypes = [ctypes.POINTER(Params), vp, vp, ctypes.c_int32, vp, ctypes.c_int32, vp, vp, vp, vp]
+        L.pod_attn_rope_table.restype = ctypes.c_int
+        L.pod_attn_rope_table.argtypes = [ctypes.POINTER(RopeParams), ctypes.POINTER(ctypes.c_uint64)]
+        L.pod_attn_append.restype = ctypes.c_int
+        L.pod_attn_append.argtypes = [ctypes.POINTER(Params), ctypes.POINTER(RopeParams), vp, ctypes.POINTER(HeadNormParams),
+                                      vp, ctypes.c_int64, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, vp, ctypes.c_int32,
+                                      vp, vp, vp, vp]
         L.pod_attn_role_for_ticket.restype = ctypes.c_int32
         L.pod_attn_role_for_ticket.argtypes = [ctypes.c_int32] * 4
         L.pod_attn_simulate_launch.restype = ctypes.c_int32
@@ -274,6 +295,29 @@ def pod_attn_forward(prefill_q: int, decode_q: int, k_cache: int, v_cache: int, 
                                   mode, vp(stream)))
 
 
+def pod_attn_build_tables(params: Params, seq_meta: int, free_blocks: int, n_free: int, block_table: int, n_rows: int,
+                          slots: int, positions: int, report: int, stream: int = 0):
+    """Blocks, slots and positions of a batch's new tokens; all tensor arguments are raw device addresses."""
+    _check(lib().pod_attn_build_tables(ctypes.byref(params), seq_meta, free_blocks, n_free, block_table, n_rows, slots,
+                                       positions, report, stream))
+
+
+def pod_attn_rope_table(rope: RopeParams) -> np.ndarray:
+    """uint64 [rot_dim / 2]: each pair's turns per position modulo 1, times 2^64 (host)."""
+    table = np.zeros(max(int(rope.rot_dim) // 2, 1), dtype=np.uint64)
+    _check(lib().pod_attn_rope_table(ctypes.byref(rope), table.ctypes.data_as(ctypes.POINTER(ctypes.c_uint64))))
+    return table
+
+
+def pod_attn_append(params: Params, rope: Optional[RopeParams], rope_table: int, norm: Optional[HeadNormParams], q: int,
+                    q_stride: int, k: int, k_stride: int, v: int, v_stride: int, slots: int, positions: int, n_rows: int,
+                    q_out: int, k_cache: int, v_cache: int, stream: int = 0):
+    """Normalise, rotate and write a batch's new tokens; all tensor arguments are raw device addresses."""
+    _check(lib().pod_attn_append(ctypes.byref(params), None if rope is None else ctypes.byref(rope), rope_table,
+                                 None if norm is None else ctypes.byref(norm), q, q_stride, k, k_stride, v, v_stride, slots,
+                                 positions, n_rows, q_out, k_cache, v_cache, stream))
+
+
 STATIC_SCRATCH_BYTES = 64 << 20
 
 
@@ -350,6 +394,136 @@ def pod_attn_simulate_launch(plan: Plan, unit_of_wg, order):
 # ----------------------------------------------------------------------------------------------
 # Convenience wrapper for torch tensors (marshalling only).
 # ----------------------------------------------------------------------------------------------
+def _on_device(dev):
+    """The device a call's tensors are on has to be the current one."""
+    import torch
+    return torch.cuda.device(dev)
+
+
+def _need(t, what, dtype, shape, device, strided=False):
+    """Raises ValueError unless t is a tensor of this type and shape on this device, in one piece (with `strided`: whose rows
+    are).  A None in the shape is any size."""
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{what} must be on {device}, not {t.device}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if not (t.is_contiguous() or (strided and (t.shape[0] == 0 or t[0].is_contiguous()))):
+        raise ValueError(f"{what} must lie in one piece" + (" row by row" if strided else ""))
+
+
+def _device(device):
+    import torch
+    device = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
+
+
+class Rope:
+    """Rotary positions: which channels turn together, how fast, and how that is stretched for long contexts.
+
+    ``scaling`` is "none", "linear", "parts" or "index" (``pod_rope_scaling``); ``trained_len``, ``low`` and ``high`` are read
+    by the last two."""
+    LAYOUTS = {"half": 0, "interleaved": 1}
+    SCALINGS = {"none": 0, "linear": 1, "parts": 2, "index": 3}
+
+    def __init__(self, rot_dim, *, layout="half", theta=10000.0, scaling="none", factor=1.0, trained_len=8192, low=1.0,
+                 high=4.0, cos_sin_scale=1.0):
+        if layout not in self.LAYOUTS or scaling not in self.SCALINGS:
+            raise ValueError(f"unknown rope layout {layout!r} or scaling {scaling!r}")
+        self.params = RopeParams(self.LAYOUTS[layout], self.SCALINGS[scaling], rot_dim, cos_sin_scale, theta, factor, trained_len,
+                                 low, high)
+        self.table = pod_attn_rope_table(self.params)
+
+
+class HeadNorm:
+    """RMS normalisation of each query and key head; a weight of None is 1, ``q`` or ``k`` False leaves those heads alone."""
+
+    def __init__(self, q_weight=None, k_weight=None, *, eps=1e-6, weight_offset=0.0, q=True, k=True):
+        self.q_weight, self.k_weight, self.eps, self.weight_offset, self.q, self.k = q_weight, k_weight, eps, weight_offset, q, k
+
+
+class TokenTables:
+    """Slots and positions of the new tokens of batches of one shape, and the blocks they take.
+
+    ``build`` may be called once per step and recorded into a graph; it fills ``slots`` and ``positions`` (int32 [n_rows],
+    rows behind the batch are padding) and ``report`` (blocks taken, blocks missing, requests refused, rows)."""
+
+    def __init__(self, params: Params, n_rows: int, *, device="cuda"):
+        import torch
+        self.params, self.n_rows, self.device = params, int(n_rows), _device(device)
+        self.slots = torch.empty(self.n_rows, dtype=torch.int32, device=self.device)
+        self.positions = torch.empty(self.n_rows, dtype=torch.int32, device=self.device)
+        self.report = torch.zeros(4, dtype=torch.int32, device=self.device)
+
+    def build(self, seq_meta, free_blocks=None, block_table=None):
+        """From seq_meta (int32 [requests, 4]); a paged cache also takes its free blocks and its block table, which is
+        written."""
+        import torch
+        p, dev = self.params, self.device
+        _need(seq_meta, "seq_meta", torch.int32, (p.n_prefill + p.n_decode, 4), dev)
+        free = table = n_free = 0
+        if p.block_size > 0:
+            _need(free_blocks, "free_blocks", torch.int32, (None,), dev)
+            _need(block_table, "block_table", torch.int32, (p.n_cache_rows, p.max_blocks_per_seq), dev)
+            free, n_free, table = free_blocks.data_ptr(), free_blocks.numel(), block_table.data_ptr()
+        with _on_device(dev):
+            pod_attn_build_tables(p, seq_meta.data_ptr(), free, n_free, table, self.n_rows, self.slots.data_ptr(),
+                                  self.positions.data_ptr(), self.report.data_ptr(), torch.cuda.current_stream(dev).cuda_stream)
+        return self
+
+
+class TokenAppend:
+    """New tokens normalised, rotated and written: queries to rows for the attention, keys and values to the cache."""
+
+    def __init__(self, params: Params, *, rope: Optional[Rope] = None, norm: Optional[HeadNorm] = None, device="cuda"):
+        import torch
+        self.params, self.device = params, _device(device)
+        self.dtype = {F16: torch.float16, BF16: torch.bfloat16}[params.dtype]
+        self.rope, self.table, self.norm = None, None, None
+        if rope is not None:
+            if rope.params.rot_dim > params.head_dim:
+                raise ValueError(f"rot_dim {rope.params.rot_dim} is more than head_dim {params.head_dim}")
+            self.rope = rope.params
+            self.table = torch.from_numpy(rope.table.view(np.int64)).to(self.device)
+        if norm is not None:
+            for name in ("q_weight", "k_weight"):
+                if getattr(norm, name) is not None:
+                    _need(getattr(norm, name), name, self.dtype, (params.head_dim,), self.device)
+            self.weights = (norm.q_weight, norm.k_weight)                # kept alive
+            ptr = lambda w: None if w is None else w.data_ptr()
+            self.norm = HeadNormParams(ptr(norm.q_weight), ptr(norm.k_weight), norm.eps, norm.weight_offset, int(norm.q), int(norm.k))
+
+    def cache_shape(self):
+        p = self.params
+        n, tokens = (p.n_blocks, p.block_size) if p.block_size > 0 else (p.n_cache_rows, p.kv_seq_stride // (p.n_kv_heads * p.head_dim))
+        return (n, p.n_kv_heads, tokens, p.head_dim) if p.kv_order == KV_HEAD_MAJOR else (n, tokens, p.n_kv_heads, p.head_dim)
+
+    def __call__(self, q, k, v, slots, positions, k_cache, v_cache, q_out=None):
+        """q, k, v: [rows, heads * head_dim] (or views of one projection); returns q_out, [rows, Hq, d]."""
+        import torch
+        p, dev, rows = self.params, self.device, slots.shape[0]
+        for t, what, heads in ((q, "q", p.n_q_heads), (k, "k", p.n_kv_heads), (v, "v", p.n_kv_heads)):
+            _need(t, what, self.dtype, (rows, heads * p.head_dim), dev, strided=True)
+        _need(slots, "slots", torch.int32, (rows,), dev)
+        _need(positions, "positions", torch.int32, (rows,), dev)
+        for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            _need(t, what, self.dtype, self.cache_shape(), dev)
+        if q_out is None:
+            q_out = torch.empty((rows, p.n_q_heads, p.head_dim), dtype=self.dtype, device=dev)
+        else:
+            _need(q_out, "q_out", self.dtype, (rows, p.n_q_heads, p.head_dim), dev)
+        if rows == 0:
+            return q_out
+        stride = lambda t: t.stride(0) if rows > 1 else t.shape[1]
+        with _on_device(dev):
+            pod_attn_append(p, self.rope, 0 if self.table is None else self.table.data_ptr(), self.norm, q.data_ptr(), stride(q),
+                            k.data_ptr(), stride(k), v.data_ptr(), stride(v), slots.data_ptr(), positions.data_ptr(), rows,
+                            q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                            torch.cuda.current_stream(dev).cuda_stream)
+        return q_out
+
+
 class HybridAttention:
     """Plan + workspace for one batch shape; ``forward`` may be called once per layer."""
 
@@ -390,6 +564,17 @@ class HybridAttention:
                          self.seq_meta_dev.data_ptr(), ptr(batch.block_table), out.data_ptr(), self.plan,
                          self.ws_ptr, self.ws_bytes, mode, stream)
         return out
+
+    def forward_tokens(self, batch, append: TokenAppend, tables: TokenTables, q, k, v, out=None, mode=MODE_FUSED):
+        """One layer of the batch from its projections: the new tokens are put into the cache at ``tables``' slots, then the
+        attention reads them.  q, k, v: [rows, heads * head_dim] in the order of the output rows; rows behind the batch are
+        padding.  The queries of ``batch`` are not read.  Returns the output rows."""
+        n = batch.n_rows
+        if q.shape[0] < n:
+            raise ValueError(f"{q.shape[0]} rows of projections for a batch of {n}")
+        rows = append(q, k, v, tables.slots, tables.positions, batch.k_cache, batch.v_cache)
+        batch = dataclasses.replace(batch, prefill_q=rows[:batch.n_prefill_rows], decode_q=rows[batch.n_prefill_rows:n])
+        return self.forward(batch, out=out, mode=mode)
 
     def enable_trace(self):
         """Allocate a trace buffer (one record per workgroup) and switch tracing on."""
