@@ -182,6 +182,37 @@ typedef struct pod_attn_plan pod_attn_plan;   /* opaque, host memory, owned by t
 pod_status pod_attn_plan_create(const pod_attn_params *params, const int32_t *seq_meta_host,
                                 pod_attn_plan **plan);
 void       pod_attn_plan_destroy(pod_attn_plan *plan);
+
+/*
+ * Scores other than plain causal ones.  With pos the position of a query's own token and j that of a key,
+ *
+ *     s_j = softmax_scale * <q, k_j>
+ *     s_j = logit_cap * tanh(s_j / logit_cap)                where logit_cap > 0
+ *     s_j = s_j - slopes[h] * |pos - j|                      where slopes are given
+ *
+ * and the query sees the keys j with first <= j < end,
+ *
+ *     first = max(0, pos - window + 1 where window > 0, doc_start[row] where given)
+ *     end   = max(pos + 1, min(prefix_len[r], kv_len) where given)
+ *
+ * i.e. a sliding window, documents that do not see each other packed into one request, and a prefix whose tokens everyone
+ * in the request sees, from in front as well.  A row with first >= end sees nothing and its result is 0.
+ * What a row does not see does not reach its result, be it infinite or NaN, and cache blocks (or parts of them) whose keys
+ * no row of the batch sees are not read: their entries in block_table may name no block.
+ */
+typedef struct {
+    float   logit_cap;          /* >= 0 and finite; 0: scores are not capped                     */
+    int32_t window;             /* >= 0; 0: no window                                             */
+    const float   *slopes;      /* host [n_q_heads], finite, or NULL                              */
+    const int32_t *doc_start;   /* host [rows of out], >= 0, or NULL                              */
+    const int32_t *prefix_len;  /* host [n_prefill + n_decode], >= 0, or NULL                     */
+} pod_attn_scores;
+
+/* pod_attn_plan_create for such scores (NULL: plain causal ones, the same plan as without).  The plan keeps what it needs of
+ * the arrays, and works with every entry point and mode but POD_MODE_FLAG_PREFILL_HEAVY (POD_ERR_UNSUPPORTED).  Work that no
+ * row sees is not planned: a window makes the work of a decode request that of its window. */
+pod_status pod_attn_plan_create_scored(const pod_attn_params *params, const pod_attn_scores *scores,
+                                       const int32_t *seq_meta_host, pod_attn_plan **plan);
 pod_status pod_attn_plan_info_get(const pod_attn_plan *plan, pod_attn_plan_info *info);
 
 /*

@@ -126,6 +126,20 @@ pod::KernelArgs make_args(const pod::Plan &p, const void *prefill_q, const void 
     return a;
 }
 
+pod::ScoredArgs make_scored(const pod::Plan &p, const pod::KernelArgs &a, const void *workspace)
+{
+    pod::ScoredArgs s;
+    static_cast<pod::KernelArgs &>(s) = a;
+    const unsigned char *ws = (const unsigned char *)workspace;
+    s.ranges = (const int32_t *)(ws + p.off_ranges);
+    s.slopes = p.slopes.empty() ? nullptr : (const float *)(ws + p.off_slopes);
+    s.zero_rows = (const int32_t *)(ws + p.off_zero_rows);
+    s.n_zero_rows = (int32_t)p.zero_rows.size();
+    s.cap_log2 = p.logit_cap * 1.4426950408889634f;
+    s.cap_exp = p.logit_cap > 0.f ? 2.f * 1.4426950408889634f * p.prm.softmax_scale / p.logit_cap : 0.f;
+    return s;
+}
+
 // The two streams the two-kernel modes run their kernels on: one pair per GPU, created when it is first
 // needed and kept until the process ends.  (A pair per plan would be spread over the few hardware queues a process
 // has in creation order, and a later plan's pair can land on one queue, where its two kernels run one after the other.
@@ -209,13 +223,16 @@ pod_status upload_tables(const pod::Plan &p, void *workspace, hipStream_t s)
     hipError_t e = pod::clear_header((pod::WsHeader *)ws, s);
     if (e != hipSuccess) return fail_hip(e, "clearing workspace counters");
     struct Part { size_t off; const void *src; size_t bytes; };
-    const Part parts[6] = {                                  // in the order they lie in
+    const Part parts[9] = {                                  // in the order they lie in
         {p.off_pitems, p.pitems.data(), p.pitems.size() * sizeof(pod::PrefillItem)},
         {p.off_pitems_by_wg, p.pitems_by_wg.data(), p.pitems_by_wg.size() * sizeof(pod::PrefillItem)},
         {p.off_pitem_of_wg, p.pitem_of_wg.data(), p.pitem_of_wg.size() * sizeof(int32_t)},
         {p.off_dunits, p.dunits.data(), p.dunits.size() * sizeof(pod::DecodeUnit)},
         {p.off_crows, p.merge_rows.data(), p.merge_rows.size() * sizeof(pod::CombineRow)},
-        {p.off_dq, p.dq_begin, sizeof p.dq_begin}};
+        {p.off_dq, p.dq_begin, sizeof p.dq_begin},
+        {p.off_ranges, p.ranges.data(), p.ranges.size() * sizeof(int32_t)},
+        {p.off_slopes, p.slopes.data(), p.slopes.size() * sizeof(float)},
+        {p.off_zero_rows, p.zero_rows.data(), p.zero_rows.size() * sizeof(int32_t)}};
     // The tables lie behind each other in the workspace: one copy.  (Six before: preparing 48 decodes + 3
     // chunks took 143 us, 95 now; 32 decodes at 32K + a chunk 181, now 128.)
     const size_t bytes = p.off_part_o - p.off_pitems;
@@ -248,6 +265,12 @@ const char *pod_attn_version(void) { return "pod_attn 0.1 (gfx950)"; }
 pod_status pod_attn_plan_create(const pod_attn_params *params, const int32_t *seq_meta_host,
                                 pod_attn_plan **plan)
 {
+    return pod_attn_plan_create_scored(params, nullptr, seq_meta_host, plan);
+}
+
+pod_status pod_attn_plan_create_scored(const pod_attn_params *params, const pod_attn_scores *scores,
+                                       const int32_t *seq_meta_host, pod_attn_plan **plan)
+{
     if (!params || !plan) return fail(POD_ERR_INVALID_ARG, "params or plan is null");
     *plan = nullptr;
     const int n_cus = params->n_compute_units > 0 ? params->n_compute_units : device_cu_count();
@@ -256,7 +279,7 @@ pod_status pod_attn_plan_create(const pod_attn_params *params, const int32_t *se
     std::string err;
     pod_status st;
     try {
-        st = pod::build_plan(*params, seq_meta_host, n_cus, obj->p, err);
+        st = pod::build_plan(*params, seq_meta_host, n_cus, obj->p, err, scores);
     } catch (const std::bad_alloc &) {
         st = POD_ERR_INVALID_ARG;
         err = "out of host memory";
@@ -403,6 +426,7 @@ static pod_status forward_impl(const void *prefill_q, const void *decode_q, cons
     if (p.prm.n_prefill > 0 && !prefill_q) return fail(POD_ERR_INVALID_ARG, "prefill_q is null");
     if (p.prm.n_decode > 0 && !decode_q) return fail(POD_ERR_INVALID_ARG, "decode_q is null");
     if (paged && !block_table) return fail(POD_ERR_INVALID_ARG, "block_table is null for a paged cache");
+    if (heavy && p.scored) return fail(POD_ERR_UNSUPPORTED, "the prefill-heavy configuration is not built for changed scores");
     if (heavy && !pod::built_for_prefill_heavy(p.prm.block_size, p.prm.head_dim, p.prm.n_kv_heads))
         return fail(POD_ERR_UNSUPPORTED, "the prefill-heavy configuration is built for head_dim 128 and contiguous or "
                                          "power-of-two (>= 16) block caches, with blocks of less than 4 GB");
@@ -448,7 +472,8 @@ static pod_status forward_impl(const void *prefill_q, const void *decode_q, cons
     hipError_t e = hipSuccess;
     auto go = [&](int which, const pod::KernelArgs &args, hipStream_t on) {
         if (which == pod::kLaunchCombine && no_combine) return;
-        if (e == hipSuccess) e = pod::launch(which, args, dt, hd, on);
+        if (e != hipSuccess) return;
+        e = p.scored ? pod::launch_scored(which, make_scored(p, args, workspace), dt, hd, on) : pod::launch(which, args, dt, hd, on);
     };
 
     // The combine pass only touches rows whose partials were produced in this call; the row list
@@ -557,6 +582,7 @@ static pod_status forward_impl(const void *prefill_q, const void *decode_q, cons
     default:
         break;
     }
+    if (!p.zero_rows.empty() && mode != POD_MODE_PREFILL_ONLY && !no_combine) go(pod::kLaunchZeroRows, a, s);
     if (e != hipSuccess) {
         if (a.combine_resets) (void)pod::clear_header(a.hdr, s);       // the combine kernel may be what failed
         return fail_hip(e, "launching attention kernels");

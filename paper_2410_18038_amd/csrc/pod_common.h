@@ -212,4 +212,15 @@ struct KernelArgs {
     float scale_log2;                      // softmax_scale * log2(e)
 };
 
+// What the kernels of plans with changed scores need besides.  Their items and units may begin at any key; what lies ahead
+// of it in the first tile or step is not read.
+struct ScoredArgs : KernelArgs {
+    const int32_t *ranges;                 // [row of out][2]: first visible key and end; first >= end: none
+    const float *slopes;                   // [n_q_heads + kMaxGroup] slope * log2(e), or null
+    float cap_log2;                        // logit_cap * log2(e); 0: not capped
+    const int32_t *zero_rows;              // decode rows that see no key
+    int32_t n_zero_rows;
+    float cap_exp;                         // 2 * log2(e) * softmax_scale / logit_cap
+};
+
 }  // namespace pod

@@ -35,6 +35,7 @@ template <> struct Num<0> {   // IEEE binary16
     using v8 = f16x8;
     using v4 = f16x4;
     using elem = _Float16;
+    static constexpr short kInf = 0x7c00, kOne = 0x3c00;       // bits of infinity and of 1
     static __device__ __forceinline__ f32x16 mfma32(v8 a, v8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
     }
@@ -55,6 +56,7 @@ template <> struct Num<1> {   // bfloat16
     using v8 = bf16x8;
     using v4 = bf16x4;
     using elem = __bf16;
+    static constexpr short kInf = 0x7f80, kOne = 0x3f80;
     static __device__ __forceinline__ f32x16 mfma32(v8 a, v8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
@@ -215,6 +217,55 @@ template <int D> struct PrefillLds {
     static constexpr int kBytes = 4 * kTileBytes;          // K[2] then V[2]
 };
 
+// Whether the arguments are those of changed scores.
+template <class A> constexpr bool kScored = std::is_same<A, ScoredArgs>::value;
+
+// Smallest of a value over the 32 query rows of a wavefront (both halves hold the same rows), in a scalar register.
+__device__ __forceinline__ int wave_min32(int x)
+{
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) x = min(x, __shfl_xor(x, d));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// What a score is multiplied by to be in units of log2(e) (1 where change_scores has done that).
+__device__ __forceinline__ float score_unit(const KernelArgs &a) { return a.scale_log2; }
+__device__ __forceinline__ float score_unit(const ScoredArgs &a) { return a.cap_log2 != 0.f || a.slopes ? 1.f : a.scale_log2; }
+
+// Score of one key in units of log2(e) from its dot product: cap * tanh(s / cap), with tanh y = 1 - 2 / (1 + e^2y).
+// (Where e^2y overflows or vanishes that is 1 or -1.)  The result is off by 2^-22 of the cap at the most.
+__device__ __forceinline__ float capped(const ScoredArgs &a, float s)
+{
+    const float e = fast_exp2(s * a.cap_exp);
+    return __builtin_fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(1.f + e), a.cap_log2);
+}
+
+// The scores of a tile in units of log2(e), from the dot products, where they are capped or fall with distance; `ahead` is
+// the distance from the row's own token to the lane's first key.
+template <int NTB>
+__device__ __forceinline__ void change_scores(const ScoredArgs &a, f32x16 (&s)[NTB], float slope, int ahead)
+{
+    if (a.cap_log2 != 0.f) {
+#pragma unroll
+        for (int tb = 0; tb < NTB; ++tb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[tb][r] = capped(a, s[tb][r]);
+    } else if (a.slopes) {
+#pragma unroll
+        for (int tb = 0; tb < NTB; ++tb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[tb][r] *= a.scale_log2;
+    }
+    if (a.slopes) {
+        const float base = (float)ahead;
+#pragma unroll
+        for (int tb = 0; tb < NTB; ++tb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[tb][r] = __builtin_fmaf(-slope, fabsf(base + (float)(tb * 32 + 8 * (r >> 2) + (r & 3))), s[tb][r]);
+    }
+}
+
 // Which chunk position of its LDS row a 16-byte chunk c of row `row` is stored at.
 template <int D> __device__ __forceinline__ int k_swizzle(int row, int c)
 {
@@ -254,10 +305,12 @@ __device__ __forceinline__ PrefillItem load_item(const PrefillItem *items, int i
     return PrefillItem{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
 }
 
-template <int DT, int D, int LAYOUT>
-__device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const PrefillItem it,
+// A is KernelArgs, or ScoredArgs for the kernels of plans whose scores are changed or masked by more than causality.
+template <int DT, int D, int LAYOUT, class A>
+__device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem it,
                                                  unsigned char *smem)
 {
+    constexpr bool SCORED = kScored<A>;
     using N = Num<DT>;
     using v8 = typename N::v8;
     using L = PrefillLds<D>;
@@ -290,16 +343,44 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
 
     // This lane's query row.
     const int R = it.row0 + rg * 32 + n32;
-    const bool row_ok = R < rows_total && (rg * 32 + n32) < it.n_rows;
+    bool row_ok = R < rows_total && (rg * 32 + n32) < it.n_rows;
     const int tok = R / group;
     const int hq = it.kv_head * group + (R - tok * group);
-    const int pos = row_ok ? prefix + tok : 0x7fffffff;    // last visible key
+    int pos = row_ok ? prefix + tok : 0x7fffffff;          // last visible key
     // Causal limits of this wavefront (rows are ordered by token).
     const int w_first = it.row0 + rg * 32;
     const int w_last = min(it.row0 + it.n_rows, it.row0 + rg * 32 + 32) - 1;
     const bool wave_has_rows = w_first < it.row0 + it.n_rows;
-    const int wave_minpos = prefix + w_first / group;
-    const int wave_maxpos = wave_has_rows ? prefix + w_last / group : -1;
+    int wave_minpos = prefix + w_first / group;
+    int wave_maxpos = wave_has_rows ? prefix + w_last / group : -1;
+    // Changed scores: the row's first visible key, the wavefront's bounds of those, the slope of the row's head.  Rows that
+    // see nothing do not take part in the bounds, and get their zeros here, from the first of the items that share the row.
+    int first = 0, wave_minfirst = 0, wave_maxfirst = 0;
+    float slope = 0.f;
+    const int key_of_row = row_ok ? prefix + tok : 0;      // where the row's own token sits
+    if constexpr (SCORED) {
+        int last = -1;
+        if (row_ok) {
+            const int32_t *range = a.ranges + 2 * (int64_t)(q_start + tok);
+            first = range[0];
+            last = range[1] - 1;
+            if (a.slopes) slope = a.slopes[hq];
+        }
+        if (row_ok && first > last && it.split == 0) {
+            typename N::elem *op = (typename N::elem *)a.out + ((int64_t)(q_start + tok) * a.n_q_heads + hq) * D;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int rq = 0; rq < 4; ++rq) *(u32x2 *)(op + (cb0 + mb) * 32 + 8 * rq + 4 * h) = u32x2{0u, 0u};
+        }
+        row_ok = first <= last;
+        pos = row_ok ? last : 0x7fffffff;
+        if (!row_ok) first = 0;
+        wave_minpos = wave_min32(row_ok ? last : 0x7fffffff);
+        wave_maxpos = -wave_min32(row_ok ? -last : 1);
+        wave_minfirst = wave_min32(row_ok ? first : 0x7fffffff);
+        wave_maxfirst = -wave_min32(row_ok ? -first : 0);
+    }
 
     v8 q[KS];
     {
@@ -361,7 +442,9 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
     const typename N::elem *vc = (const typename N::elem *)a.v_cache + it.kv_head * a.head_stride;
     const POD_CONST int32_t *table = (const POD_CONST int32_t *)a.block_table +
                                      (int64_t)cache_row * a.max_blocks_per_seq;
-    const int n_tiles = (it.kv_end - it.kv_begin + T - 1) / T;
+    // Keys are staged from a multiple of 16 on: the first key that a row sees may lie behind it.
+    const int kv_base = SCORED ? it.kv_begin & ~15 : it.kv_begin;
+    const int n_tiles = (it.kv_end - kv_base + T - 1) / T;
 
     // Byte offsets (from the start of the cache, K/V head 0) of the rows each pass of this
     // wavefront loads, for a full tile: one uniform 64-bit value per pass.  For the paged layout
@@ -378,14 +461,14 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
         TileBlocks tb;
         if constexpr (LAYOUT == kLayoutPaged16) {
             if (D == 128 && blocks16) {
-                const int i0 = min((it.kv_begin + jt * T) >> 4, a.max_blocks_per_seq - 4);
+                const int i0 = min((kv_base + jt * T) >> 4, a.max_blocks_per_seq - 4);
                 const i32x4_a4 ids = *(const POD_CONST i32x4_a4 *)(table + i0);
 #pragma unroll
                 for (int p = 0; p < NPASS; ++p) tb.id[p] = ids[p & 3];
             } else {
 #pragma unroll
                 for (int p = 0; p < NPASS; ++p) {
-                    const int t = min(it.kv_begin + jt * T + p * RPP + wave * RPW, it.kv_end - 1);
+                    const int t = min(kv_base + jt * T + p * RPP + wave * RPW, it.kv_end - 1);
                     tb.id[p] = table[t >> a.bs_shift];
                 }
             }
@@ -393,7 +476,7 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
 #pragma unroll
             for (int p = 0; p < NPASS; ++p) {
                 int off;
-                tb.id[p] = table[block_of(a, min(it.kv_begin + jt * T + p * RPP + wave * RPW, it.kv_end - 1), off)];
+                tb.id[p] = table[block_of(a, min(kv_base + jt * T + p * RPP + wave * RPW, it.kv_end - 1), off)];
             }
         } else {
 #pragma unroll
@@ -403,7 +486,7 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
     };
     auto tile_bases = [&](int jt, const TileBlocks &blk) {
         TileBases tb;
-        const int j0 = it.kv_begin + jt * T;
+        const int j0 = kv_base + jt * T;
         if constexpr (LAYOUT == kLayoutContiguous) {
             const int64_t off = ((int64_t)cache_row * a.kv_seq_stride + (int64_t)j0 * token_elems) * 2;
 #pragma unroll
@@ -443,22 +526,27 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
         }
     };
     auto tile_is_fast = [&](int jt) {
-        return LAYOUT != kLayoutPagedAny && it.kv_end - (it.kv_begin + jt * T) >= T;
+        if (SCORED && jt == 0 && kv_base != it.kv_begin) return false;
+        return LAYOUT != kLayoutPagedAny && it.kv_end - (kv_base + jt * T) >= T;
     };
 
     // General path: any layout, and the last tile of an item when it is not full.  Rows past the
-    // item's last key re-read its last row: finite data, masked out of the softmax by index.
+    // item's last key re-read its last row: finite data, masked out of the softmax by index.  (Rows ahead of the
+    // first key re-read that one: what lies there may be no row of the cache any more.)
     auto issue_tile = [&](int jt, int buf, bool want_k, bool want_v) {
-        const int j0 = it.kv_begin + jt * T;
+        const int j0 = kv_base + jt * T;
         const int last_row = it.kv_end - 1 - j0;                // >= 0
+        const int first_row = SCORED ? max(it.kv_begin - j0, 0) : 0;
 #pragma unroll
         for (int p = 0; p < NPASS; ++p) {
             const int row_base = p * RPP + wave * RPW;           // uniform
-            const int base_eff = min(row_base, last_row & ~(RPW - 1));
+            int base_eff = min(row_base, last_row & ~(RPW - 1));
+            if constexpr (SCORED) base_eff = max(base_eff, first_row & ~(RPW - 1));
             const uint32_t dst_k = lds0 + (uint32_t)(buf * L::kTileBytes + (p * kWgThreads + wave * kWaveSize) * 16);
             const uint32_t dst_v = dst_k + 2 * L::kTileBytes;
             if constexpr (LAYOUT == kLayoutPagedAny) {
-                const int row = min(row_base + wr_row, last_row);
+                int row = min(row_base + wr_row, last_row);
+                if constexpr (SCORED) row = max(row, first_row);
                 const int64_t off = token_offset<true>(a, cache_row, j0 + row, token_elems);
                 const int lrow = row_base + wr_row;              // swizzle follows the LDS row
                 if (want_k) dma16_vaddr(dst_k, kc + off + k_swizzle<D>(lrow, wr_pos) * 8);
@@ -477,7 +565,8 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
                     base = (int64_t)blk * a.block_elems + (int64_t)off * token_elems;
                 }
                 const int lrow = row_base + wr_row;
-                const int rl = min(lrow, last_row) - base_eff;
+                int rl = min(lrow, last_row) - base_eff;
+                if constexpr (SCORED) rl = max(min(lrow, last_row), first_row) - base_eff;
                 const uint32_t ko = (uint32_t)(rl * token_elems + k_swizzle<D>(lrow, wr_pos) * 8) * 2u;
                 const uint32_t vo = (uint32_t)(rl * token_elems + v_swizzle<D>(lrow, wr_pos) * 8) * 2u;
                 if (want_k) dma16(dst_k, ko, kc + base);
@@ -493,7 +582,7 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
         for (int r = 0; r < 16; ++r) o[mb][r] = 0.f;
     float m_run = neg_inf();
     f32x4 l_run = {0.f, 0.f, 0.f, 0.f};                      // four copies of this lane's weight sum
-    const float c = a.scale_log2;
+    const float c = score_unit(a);
 
     // S^T = K Q^T for one tile: rows = keys, columns = this wavefront's query rows.
     // Register r of block tb holds key j0 + tb*32 + 8*(r/4) + 4*h + r%4.
@@ -530,7 +619,7 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
         __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
     };
 
-    if (n_tiles <= 0) return;                                // never planned; keeps the loop simple
+    if (n_tiles <= 0) return;                                // a block of rows that see nothing (or never planned)
     __syncthreads();                                         // previous use of this LDS is over
     TileBases carry = {};                                     // bases of tile jt+1 inside the loop
     if (tile_is_fast(0)) {
@@ -560,12 +649,12 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
     // and odd tiles) so that the swap is a matter of names, not of 32 register moves per tile, and
     // the LDS buffer of a tile is known at compile time.
     f32x16 s_even[NTB], s_odd[NTB];
-    if (it.kv_begin <= wave_maxpos) scores(0, s_even);
+    if (kv_base <= wave_maxpos && (!SCORED || kv_base + T > wave_minfirst)) scores(0, s_even);
     __syncthreads();                                         // K tile 0 is free to be overwritten
 
     auto tile_step = [&](const int jt, auto parity, f32x16 (&s_cur)[NTB], f32x16 (&s_next)[NTB])
                          __attribute__((always_inline)) {
-        const int j0 = it.kv_begin + jt * T;
+        const int j0 = kv_base + jt * T;
         constexpr int cur = decltype(parity)::value;
         // K tile jt was consumed in the previous iteration and V tile jt-1 as well (barrier below).
         TileBases fresh = carry;
@@ -584,8 +673,12 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
         carry = fresh;
         blocks_ahead = tile_blocks(jt + 3);                  // used by the next iteration
 
-        const bool live = j0 <= wave_maxpos;                 // something visible to this wavefront
-        const bool next_live = (jt + 1 < n_tiles) && (j0 + T <= wave_maxpos);
+        bool live = j0 <= wave_maxpos;                       // something visible to this wavefront
+        bool next_live = (jt + 1 < n_tiles) && (j0 + T <= wave_maxpos);
+        if constexpr (SCORED) {
+            live = live && j0 + T > wave_minfirst;
+            next_live = next_live && j0 + 2 * T > wave_minfirst;
+        }
         // Matrix blocks ask for issue before the other wavefront's softmax: the two then settle into
         // opposite phases.  (At 256 channels raised priority costs the decode stream more; see the worker.)
         if constexpr (D <= 128) __builtin_amdgcn_s_setprio(3);
@@ -593,7 +686,11 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
         if constexpr (D <= 128) __builtin_amdgcn_s_setprio(2);
         if (live) {
             // vector ALUs: softmax of the current tile
-            const bool need_mask = (j0 + T - 1 > wave_minpos) || (j0 + T > it.kv_end);
+            bool need_mask = (j0 + T - 1 > wave_minpos) || (j0 + T > it.kv_end);
+            if constexpr (SCORED) {
+                need_mask = need_mask || j0 < wave_maxfirst;
+                change_scores(a, s_cur, slope, j0 + 4 * h - key_of_row);
+            }
             if (__builtin_expect(need_mask, 0)) {
                 const int lim = min(pos, it.kv_end - 1);
 #pragma unroll
@@ -601,7 +698,7 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int key = j0 + tb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-                        if (key > lim) s_cur[tb][r] = neg_inf();
+                        if (key > lim || (SCORED && key < first)) s_cur[tb][r] = neg_inf();
                     }
             }
             float mx = neg_inf();
@@ -681,6 +778,102 @@ __device__ __forceinline__ void prefill_item_run(const KernelArgs &a, const Pref
         tile_step(jt, std::integral_constant<int, 0>{}, s_even, s_odd);
         if (jt + 1 >= n_tiles) break;
         tile_step(jt + 1, std::integral_constant<int, 1>{}, s_odd, s_even);
+    }
+
+    // A weight of 0 does not keep out what is no number: a value that a row does not see, but others of its tile do, may be
+    // infinite or NaN, and has then made the row's sums NaN.  Where a row of the workgroup has sums that are not finite the
+    // item is done again, a tile at a time, with such values taken out of the product and given to the rows that see
+    // them: +inf, -inf or both (NaN).  (Kept out of the loop above, which has no registers left for it.)
+    if constexpr (SCORED) {
+        float finite = 0.f;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) finite = __builtin_fmaf(o[mb][r], 0.f, finite);
+        POD_LDS uint32_t *const votes = (POD_LDS uint32_t *)lds;
+        const uint32_t odd = __builtin_amdgcn_ballot_w64(row_ok && finite != 0.f) != 0;      // (NaN is not 0)
+        if (lane == 0) votes[wave] = odd;
+        __syncthreads();
+        const uint32_t any = votes[0] | votes[1] | votes[2] | votes[3];
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(any) != 0, 0)) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[mb][r] = 0.f;
+            m_run = neg_inf();
+            l_run = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int lim = min(pos, it.kv_end - 1);
+#pragma unroll 1
+            for (int jt = 0; jt < n_tiles; ++jt) {
+                const int j0 = kv_base + jt * T;
+                __syncthreads();
+                issue_tile(jt, 0, true, true);
+                wait_all_loads();
+                __syncthreads();
+                if (j0 > wave_maxpos || j0 + T <= wave_minfirst) continue;
+                f32x16 s[NTB];
+                scores(0, s);
+                change_scores(a, s, slope, j0 + 4 * h - key_of_row);
+                float mx = neg_inf();
+#pragma unroll
+                for (int tb = 0; tb < NTB; ++tb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = j0 + tb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+                        if (key > lim || key < first) s[tb][r] = neg_inf();
+                        mx = fmaxf(mx, s[tb][r]);
+                    }
+                mx = max_across_32(mx) * c;
+                const float m_new = fmaxf(m_run, mx), m_use = m_new == neg_inf() ? 0.f : m_new;
+                const float alpha = fast_exp2(m_run - m_use);
+                m_run = m_new;
+                l_run = l_run * alpha;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[mb][r] *= alpha;
+#pragma unroll 1
+                for (int half = 0; half < 2 * NTB; ++half) {          // 16 keys: half a register block of scores
+                    s16x8 p, seen;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float x = s[0][e];
+#pragma unroll
+                        for (int k = 1; k < 2 * NTB; ++k) x = half == k ? s[k >> 1][(k & 1) * 8 + e] : x;
+                        p[e] = __builtin_bit_cast(short, (typename N::elem)fast_exp2(__builtin_fmaf(x, c, -m_use)));
+                        const int key = j0 + 16 * half + 8 * (e >> 2) + 4 * h + (e & 3);
+                        seen[e] = key <= lim && key >= first ? N::kOne : (short)0;
+                    }
+                    const u32x4 pw = __builtin_bit_cast(u32x4, p);
+                    l_run = N::add_all(u32x2{pw[0], pw[1]}, l_run);
+                    l_run = N::add_all(u32x2{pw[2], pw[3]}, l_run);
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) {
+                        const POD_LDS unsigned char *vp = lds + 2 * L::kTileBytes + 16 * half * L::kRowBytes + (v_rd0 ^ (uint32_t)((cb0 + mb) << 6));
+                        const s16x8 v = __builtin_shufflevector(lds_read_tr(vp), lds_read_tr(vp + 8 * L::kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7);
+                        s16x8 number, above, below;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const bool odd_value = (v[e] & N::kInf) == N::kInf, nan = odd_value && (v[e] & 0x7fff) != N::kInf;
+                            number[e] = odd_value ? (short)0 : v[e];
+                            above[e] = odd_value && (nan || v[e] >= 0) ? N::kOne : (short)0;
+                            below[e] = odd_value && (nan || v[e] < 0) ? N::kOne : (short)0;
+                        }
+                        f32x16 ups, downs;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) ups[r] = downs[r] = 0.f;
+                        o[mb] = N::mfma32(__builtin_bit_cast(v8, number), __builtin_bit_cast(v8, p), o[mb]);
+                        ups = N::mfma32(__builtin_bit_cast(v8, above), __builtin_bit_cast(v8, seen), ups);
+                        downs = N::mfma32(__builtin_bit_cast(v8, below), __builtin_bit_cast(v8, seen), downs);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            if (ups[r] > 0.f) o[mb][r] += __builtin_inff();
+                            if (downs[r] > 0.f) o[mb][r] -= __builtin_inff();
+                        }
+                    }
+                }
+            }
+        }
     }
 
     // Epilogue.  o[mb][r] is channel (cb0 + mb)*32 + 8*(r/4) + 4*h + r%4 of this lane's query row.
@@ -910,10 +1103,11 @@ __device__ __forceinline__ void merge_if_last(const KernelArgs &a, POD_LDS unsig
 // merges it.  Kernels of plans that do not are built without that code: jumped over, its 750 instructions still cost
 // launches of 20-25 us 0.4-0.6 us, prefill roles included (126 decodes of up to 192 keys beside three short chunks,
 // 32 / 4 heads, 20.0 / 19.4 us with / without it; 80 of them, 32 / 8 heads, 26.3 / 25.7).
-template <int DT, int D, int LAYOUT, bool MERGE>
-__device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned char *smem, const int seat,
+template <int DT, int D, int LAYOUT, bool MERGE, class A>
+__device__ __forceinline__ int decode_worker_run(const A &a, unsigned char *smem, const int seat,
                                                  const int xcd)
 {
+    constexpr bool SCORED = kScored<A>;
     using N = Num<DT>;
     using v8 = typename N::v8;
     using elem = typename N::elem;
@@ -936,7 +1130,7 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
     const int group = a.group;
     const int token_elems = a.tok_stride;           // elements between consecutive tokens of a head
     const bool col_ok = n16 < group;
-    const float c = a.scale_log2;
+    const float c = score_unit(a);
     const int ld_row = lane / CH, ld_chunk = lane % CH;
     POD_LDS unsigned char *const lds_k = (POD_LDS unsigned char *)(smem + wave * L::kBytesPerWave);
     POD_LDS unsigned char *const lds_v = lds_k + L::kKBytes;
@@ -945,13 +1139,16 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
 
     // Unit descriptors and everything derived from them are wavefront-uniform: they are read
     // through the constant address space so that they live in scalar registers.
-    struct Desc { int id, kv_head, t0, t1, prow0, q_start, cache_row; };
+    struct PlainDesc { int id, kv_head, t0, t1, prow0, q_start, cache_row; };
+    struct ScoredDesc : PlainDesc { int req; };
+    using Desc = typename std::conditional<SCORED, ScoredDesc, PlainDesc>::type;
     auto load_desc = [&](int idx) __attribute__((always_inline)) -> Desc {
         idx = __builtin_amdgcn_readfirstlane(idx);
         const POD_CONST int32_t *w = (const POD_CONST int32_t *)a.dunits + 8 * (int64_t)idx;
         Desc d;
         d.id = idx;
         d.kv_head = w[1]; d.t0 = w[2]; d.t1 = w[3]; d.prow0 = w[4]; d.q_start = w[6]; d.cache_row = w[7];
+        if constexpr (SCORED) d.req = w[0];
         return d;
     };
 
@@ -1063,14 +1260,19 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
     const POD_CONST int32_t *table = nullptr;
     int n_iss = 0, q_mark = 0;                     // steps issued so far; their count when the last Q copy was issued
 
+    // Least value of the first row of a load: the one that holds the unit's first key.
+    auto first_load = [&](int t_first) __attribute__((always_inline)) { return max(hu.t0 - t_first, 0) & ~(RPI - 1); };
     // Rows past the end of a unit's last step re-read its last row (the keys are masked out of the
-    // softmax by index), so every load is in bounds and none sits behind a branch.
+    // softmax by index), so every load is in bounds and none sits behind a branch.  (With changed scores a unit's first
+    // key may lie inside its first step, and the rows ahead of it re-read its row.)
     auto set_voff = [&](int t_first, int t1) __attribute__((always_inline)) {
         const int last_row = min(t1 - 1 - t_first, STEP - 1);
 #pragma unroll
         for (int p = 0; p < NLD; ++p) {
             int row = min(p * RPI + ld_row, last_row);
-            if constexpr (LAYOUT == kLayoutPagedRows) row -= min(p * RPI, last_row & ~(RPI - 1));
+            if constexpr (SCORED) row = max(row, hu.t0 - t_first);
+            if constexpr (LAYOUT == kLayoutPagedRows && SCORED) row -= max(min(p * RPI, last_row & ~(RPI - 1)), first_load(t_first));
+            else if constexpr (LAYOUT == kLayoutPagedRows) row -= min(p * RPI, last_row & ~(RPI - 1));
             voff[p] = (uint32_t)(row * token_elems + ld_chunk * 8) * 2u;
         }
     };
@@ -1087,20 +1289,24 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
             const int last_row = min(t1 - 1 - t, STEP - 1);
             int blk[NLD], off[NLD];
 #pragma unroll
-            for (int p = 0; p < NLD; ++p) blk[p] = table[block_of(a, t + min(p * RPI, last_row & ~(RPI - 1)), off[p])];
+            for (int p = 0; p < NLD; ++p) {
+                if constexpr (SCORED) blk[p] = table[block_of(a, t + max(min(p * RPI, last_row & ~(RPI - 1)), first_load(t)), off[p])];
+                else blk[p] = table[block_of(a, t + min(p * RPI, last_row & ~(RPI - 1)), off[p])];
+            }
 #pragma unroll
             for (int p = 0; p < NLD; ++p) h_base[p] = (int64_t)blk[p] * a.block_elems + (int64_t)off[p] * token_elems;
         }
     };
     auto set_head = [&](const Desc &d) __attribute__((always_inline)) {
         hu = d;
-        h_t = d.t0;
-        h_addr_t = d.t0;
+        const int t0 = SCORED ? d.t0 & ~(STEP - 1) : d.t0;
+        h_t = t0;
+        h_addr_t = t0;
         kc = (const elem *)a.k_cache + d.kv_head * a.head_stride;
         vc = (const elem *)a.v_cache + d.kv_head * a.head_stride;
         table = (const POD_CONST int32_t *)a.block_table + (int64_t)d.cache_row * a.max_blocks_per_seq;
-        set_base(d.cache_row, d.t0, d.t1);
-        set_voff(d.t0, d.t1);
+        set_base(d.cache_row, t0, d.t1);
+        set_voff(t0, d.t1);
     };
 
     struct Slot { u32x4 k[NLD], v[NLD]; };
@@ -1112,7 +1318,8 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
             const int last_row = hu.t1 - 1 - h_addr_t;       // >= 0
 #pragma unroll
             for (int p = 0; p < NLD; ++p) {
-                const int row = min(p * RPI + ld_row, last_row);
+                int row = min(p * RPI + ld_row, last_row);
+                if constexpr (SCORED) row = max(row, hu.t0 - h_addr_t);
                 const int64_t off = token_offset<true>(a, hu.cache_row, h_addr_t + row, token_elems) + ld_chunk * 8;
                 sl.k[p] = load16_stream(kc + off);
                 sl.v[p] = load16_stream(vc + off);
@@ -1135,7 +1342,7 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
                 h_addr_t = h_t;
                 if constexpr (LAYOUT == kLayoutContiguous) h_base[0] += (int64_t)STEP * token_elems;
                 else set_base(hu.cache_row, h_t, hu.t1);
-                if (h_t + STEP > hu.t1) set_voff(h_t, hu.t1);     // ragged last step
+                if (h_t + STEP > hu.t1 || (SCORED && h_t - STEP < hu.t0)) set_voff(h_t, hu.t1);     // ragged last step (or first one before)
             }
         }
     };
@@ -1159,6 +1366,22 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
     };
 
     // ---- tail: the step being computed ------------------------------------------------------------
+    // Changed scores: the slope of the lane's head and where the unit's own token sits.  (Scalar loads: a vector load here
+    // would be one more in flight than the ring's waits count on.)
+    float slope = 0.f;
+    int key_of_row = 0;
+    auto enter_unit = [&](const Desc &d) __attribute__((always_inline)) {
+        if constexpr (SCORED) {
+            if (a.slopes) {
+                const POD_CONST float *sl = (const POD_CONST float *)a.slopes + d.kv_head * group;
+                float x = 0.f;
+#pragma unroll
+                for (int g = 0; g < kMaxGroup; ++g) x = n16 == g ? sl[g] : x;    // (kMaxGroup more are there than heads)
+                slope = x;
+                key_of_row = ((const POD_CONST int32_t *)a.seq_meta)[4 * d.req + 2] - 1;
+            }
+        }
+    };
     f32x4 o[MB];
     float m_run, l_run;
     auto reset_acc = [&]() __attribute__((always_inline)) {
@@ -1184,6 +1407,17 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
             s = N::mfma16(kk, q[ks], s);
         }
         const int n_valid = min(cu.t1 - t_first, STEP) - 4 * b4;         // keys of this lane that exist
+        if constexpr (SCORED) {
+            const int n_ahead = cu.t0 - t_first - 4 * b4;                // ... of which these are ahead of the unit's first key
+            const float base = (float)(t_first + 4 * b4 - key_of_row);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (a.cap_log2 != 0.f) s[r] = capped(a, s[r]);
+                else if (a.slopes) s[r] *= a.scale_log2;
+                if (a.slopes) s[r] = __builtin_fmaf(-slope, fabsf(base + (float)r), s[r]);
+                s[r] = (r >= n_ahead) ? s[r] : neg_inf();
+            }
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[r] = (r < n_valid) ? s[r] : neg_inf();
         float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
@@ -1265,6 +1499,7 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
         if (idx0 < 0 || idx0 >= a.n_dunits) return 0;
         set_head(load_desc(idx0));
         cu = hu;
+        enter_unit(cu);
         q_dma(cu, 0);
     }
     uint64_t tb = a.evlog ? wall_clock64() : 0;
@@ -1322,6 +1557,7 @@ __device__ __forceinline__ int decode_worker_run(const KernelArgs &a, unsigned c
                     st &= ~kNextValid;
                 }
                 cu = hu;
+                enter_unit(cu);
                 st |= kHeadInTail;
                 if (n_iss - q_mark < R) wait_all_loads();    // the query copy may still be in flight
                 q_cur ^= 1;
@@ -1345,8 +1581,8 @@ template <int D> struct FusedLds {
 // Stand-alone kernels: the in-house serial and two-stream baselines (Section 3.1), and what a
 // batch with one operation runs.
 // ------------------------------------------------------------------------------------------
-template <int DT, int D, int LAYOUT>
-__global__ __launch_bounds__(kWgThreads, 2) void prefill_kernel(KernelArgs a)
+template <int DT, int D, int LAYOUT, class A>
+__device__ __forceinline__ void prefill_workgroup(const A a)
 {
     __shared__ __attribute__((aligned(16))) unsigned char smem[PrefillLds<D>::kBytes];
     const uint64_t t0 = a.trace || a.evlog ? wall_clock64() : 0;
@@ -1355,12 +1591,14 @@ __global__ __launch_bounds__(kWgThreads, 2) void prefill_kernel(KernelArgs a)
     if (a.trace && threadIdx.x == 0)
         write_trace(a, blockIdx.x, __smid() & (kCuSlots - 1), kPrefill, 1, 0, t0, wall_clock64());
 }
+template <int DT, int D, int LAYOUT>
+__global__ __launch_bounds__(kWgThreads, 2) void prefill_kernel(KernelArgs a) { prefill_workgroup<DT, D, LAYOUT>(a); }
 
 // A prefill worker: the workgroup claims prefill items until none is left, first from the queue
 // of the XCD it runs on (the items of a K/V head sit in one queue, so their K/V tiles are re-read
 // from that XCD's L2), then from the other XCDs' queues.
-template <int DT, int D, int LAYOUT>
-__device__ __forceinline__ int prefill_worker_run(const KernelArgs &a, unsigned char *smem, int *slot, int xcd)
+template <int DT, int D, int LAYOUT, class A>
+__device__ __forceinline__ int prefill_worker_run(const A &a, unsigned char *smem, int *slot, int xcd)
 {
     int n_done = 0;
     int q = xcd & (kXcdQueues - 1);
@@ -1438,8 +1676,8 @@ __device__ __forceinline__ void finish_and_reset(const KernelArgs &a, int *flag)
     if (*flag) reset_counters(hdr);
 }
 
-template <int DT, int D, int LAYOUT, bool MERGE>
-__device__ __forceinline__ void decode_workgroup(const KernelArgs a)
+template <int DT, int D, int LAYOUT, bool MERGE, class A>
+__device__ __forceinline__ void decode_workgroup(const A a)
 {
     __shared__ __attribute__((aligned(16))) unsigned char smem[DecodeLds<D>::kBytes];
     __shared__ int flag;
@@ -1755,8 +1993,8 @@ __global__ __launch_bounds__(kWgThreads, 2) __attribute__((amdgpu_num_vgpr(kHeav
 // one item at a time; as a decode worker each of its wavefronts takes units on its own
 // (Section 4.2.3).  No workgroup ever waits for another one.
 // ------------------------------------------------------------------------------------------
-template <int DT, int D, int LAYOUT, bool MERGE>
-__device__ __forceinline__ void fused_workgroup(const KernelArgs a)
+template <int DT, int D, int LAYOUT, bool MERGE, class A>
+__device__ __forceinline__ void fused_workgroup(const A a)
 {
     __shared__ __attribute__((aligned(16))) unsigned char smem[FusedLds<D>::kBytes];
     __shared__ int bind[6];                                  // role, seat, unit id, last flag, item, queue
@@ -1817,8 +2055,8 @@ __global__ __launch_bounds__(kWgThreads, 2) void fused_merging(KernelArgs a) { f
 // It is also the kernel of launches whose work is all resident at once (fixed_roles): operation and piece
 // of work then follow from the workgroup index, and only decode units beyond the fixed ones are claimed.
 // ------------------------------------------------------------------------------------------
-template <int DT, int D, int LAYOUT, bool MERGE>
-__device__ __forceinline__ void fused_cta_workgroup(const KernelArgs a)
+template <int DT, int D, int LAYOUT, bool MERGE, class A>
+__device__ __forceinline__ void fused_cta_workgroup(const A a)
 {
     __shared__ __attribute__((aligned(16))) unsigned char smem[FusedLds<D>::kBytes];
     __shared__ int bind[4];                                  // role, work id, unit id, last flag
@@ -1968,6 +2206,27 @@ __global__ __launch_bounds__(kWgThreads) void combine_kernel(KernelArgs a)
 }
 
 // ------------------------------------------------------------------------------------------
+// The kernels of plans with changed scores: the same workgroups with the scores capped, falling with distance or masked by
+// an interval of keys per row.
+// ------------------------------------------------------------------------------------------
+template <int DT, int D, int LAYOUT>
+__global__ __launch_bounds__(kWgThreads, 2) void prefill_scored(ScoredArgs a) { prefill_workgroup<DT, D, LAYOUT, const ScoredArgs &>(a); }
+template <int DT, int D, int LAYOUT>
+__global__ __launch_bounds__(kWgThreads, 2) void decode_scored(ScoredArgs a) { decode_workgroup<DT, D, LAYOUT, false, const ScoredArgs &>(a); }
+template <int DT, int D, int LAYOUT>
+__global__ __launch_bounds__(kWgThreads, 2) void fused_scored(ScoredArgs a) { fused_workgroup<DT, D, LAYOUT, false, const ScoredArgs &>(a); }
+template <int DT, int D, int LAYOUT>
+__global__ __launch_bounds__(kWgThreads, 2) void fused_cta_scored(ScoredArgs a) { fused_cta_workgroup<DT, D, LAYOUT, false, const ScoredArgs &>(a); }
+// Decode rows that see no key have no unit; their results are zeros.  (16 bytes a thread, a row a workgroup.)
+template <int D>
+__global__ __launch_bounds__(kWgThreads) void zero_decode_rows(void *out, const int32_t *rows, int64_t first_row, int n_q_heads)
+{
+    const int row_pieces = n_q_heads * (D / 8);
+    u32x4 *to = (u32x4 *)out + (first_row + rows[blockIdx.x]) * row_pieces;
+    for (int i = threadIdx.x; i < row_pieces; i += kWgThreads) to[i] = u32x4{0u, 0u, 0u, 0u};
+}
+
+// ------------------------------------------------------------------------------------------
 // Host-side launchers.
 // ------------------------------------------------------------------------------------------
 template <int DT, int D, int LAYOUT>
@@ -2041,6 +2300,45 @@ static hipError_t launch_variant(int which, const KernelArgs &a, hipStream_t str
     return hipGetLastError();
 }
 
+template <int DT, int D, int LAYOUT>
+static hipError_t launch_scored_variant(int which, const ScoredArgs &a, hipStream_t stream)
+{
+    const dim3 threads(kWgThreads);
+    switch (which) {
+    case kLaunchPrefill:
+        if (a.n_pitems > 0) prefill_scored<DT, D, LAYOUT><<<dim3(a.n_pitems), threads, 0, stream>>>(a);
+        break;
+    case kLaunchDecode:
+        if (a.n_dwgs > 0) decode_scored<DT, D, LAYOUT><<<dim3(a.n_dwgs), threads, 0, stream>>>(a);
+        break;
+    case kLaunchFused:
+        if (a.fused_grid > 0) fused_scored<DT, D, LAYOUT><<<dim3(a.fused_grid), threads, 0, stream>>>(a);
+        break;
+    case kLaunchFusedCta:
+        if (a.n_pitems + a.n_dctas > 0) fused_cta_scored<DT, D, LAYOUT><<<dim3(a.n_pitems + a.n_dctas), threads, 0, stream>>>(a);
+        break;
+    case kLaunchZeroRows:
+        if (a.n_zero_rows > 0)
+            zero_decode_rows<D><<<dim3(a.n_zero_rows), threads, 0, stream>>>(a.out, a.zero_rows, a.n_prefill_rows, a.n_q_heads);
+        break;
+    default:
+        return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+template <int DT, int D>
+hipError_t launch_scored_layout(int which, const ScoredArgs &a, int layout, hipStream_t stream)
+{
+    switch (layout) {
+    case kLayoutContiguous: return launch_scored_variant<DT, D, kLayoutContiguous>(which, a, stream);
+    case kLayoutPaged16: return launch_scored_variant<DT, D, kLayoutPaged16>(which, a, stream);
+    case kLayoutPagedRows: return launch_scored_variant<DT, D, kLayoutPagedRows>(which, a, stream);
+    case kLayoutPagedAny: return launch_scored_variant<DT, D, kLayoutPagedAny>(which, a, stream);
+    default: return hipErrorInvalidValue;
+    }
+}
+
 template <int DT, int D>
 hipError_t launch_layout(int which, const KernelArgs &a, int layout, hipStream_t stream)
 {
@@ -2053,9 +2351,11 @@ hipError_t launch_layout(int which, const KernelArgs &a, int layout, hipStream_t
     }
 }
 
-// This file is compiled once per (16-bit type, head_dim), which holds the kernels of that pair, and
-// once without, which holds the rest: the compilations run side by side.
-#if defined(POD_INSTANCE_DT)
+// This file is compiled twice per (16-bit type, head_dim), which hold the kernels of that pair and those of changed
+// scores, and once without, which holds the rest: the compilations run side by side.
+#if defined(POD_INSTANCE_SCORED)
+template hipError_t launch_scored_layout<POD_INSTANCE_DT, POD_INSTANCE_D>(int, const ScoredArgs &, int, hipStream_t);
+#elif defined(POD_INSTANCE_DT)
 template hipError_t launch_layout<POD_INSTANCE_DT, POD_INSTANCE_D>(int, const KernelArgs &, int, hipStream_t);
 #else
 extern template hipError_t launch_layout<0, 64>(int, const KernelArgs &, int, hipStream_t);
@@ -2064,6 +2364,26 @@ extern template hipError_t launch_layout<0, 256>(int, const KernelArgs &, int, h
 extern template hipError_t launch_layout<1, 64>(int, const KernelArgs &, int, hipStream_t);
 extern template hipError_t launch_layout<1, 128>(int, const KernelArgs &, int, hipStream_t);
 extern template hipError_t launch_layout<1, 256>(int, const KernelArgs &, int, hipStream_t);
+
+extern template hipError_t launch_scored_layout<0, 64>(int, const ScoredArgs &, int, hipStream_t);
+extern template hipError_t launch_scored_layout<0, 128>(int, const ScoredArgs &, int, hipStream_t);
+extern template hipError_t launch_scored_layout<0, 256>(int, const ScoredArgs &, int, hipStream_t);
+extern template hipError_t launch_scored_layout<1, 64>(int, const ScoredArgs &, int, hipStream_t);
+extern template hipError_t launch_scored_layout<1, 128>(int, const ScoredArgs &, int, hipStream_t);
+extern template hipError_t launch_scored_layout<1, 256>(int, const ScoredArgs &, int, hipStream_t);
+
+hipError_t launch_scored(int which, const ScoredArgs &a, int dtype, int head_dim, hipStream_t stream)
+{
+    if (which == kLaunchCombine) return launch(which, a, dtype, head_dim, stream);
+    const int layout = cache_layout(a.block_size, head_dim, a.n_kv_heads);
+    if (dtype == 0 && head_dim == 128) return launch_scored_layout<0, 128>(which, a, layout, stream);
+    if (dtype == 0 && head_dim == 64) return launch_scored_layout<0, 64>(which, a, layout, stream);
+    if (dtype == 1 && head_dim == 128) return launch_scored_layout<1, 128>(which, a, layout, stream);
+    if (dtype == 1 && head_dim == 64) return launch_scored_layout<1, 64>(which, a, layout, stream);
+    if (dtype == 0 && head_dim == 256) return launch_scored_layout<0, 256>(which, a, layout, stream);
+    if (dtype == 1 && head_dim == 256) return launch_scored_layout<1, 256>(which, a, layout, stream);
+    return hipErrorInvalidValue;
+}
 
 __global__ void clear_header_kernel(WsHeader *hdr)
 {

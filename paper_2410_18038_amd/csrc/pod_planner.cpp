@@ -54,6 +54,9 @@ size_t lay_out(Plan &plan, size_t n_pitems, size_t n_dunits, size_t n_merge_rows
     plan.off_dunits = off;   off = align256(off + n_dunits * sizeof(DecodeUnit));
     plan.off_crows = off;    off = align256(off + n_merge_rows * sizeof(CombineRow));
     plan.off_dq = off;       off = align256(off + sizeof plan.dq_begin);
+    plan.off_ranges = off;   off = align256(off + plan.ranges.size() * sizeof(int32_t));
+    plan.off_slopes = off;   off = align256(off + plan.slopes.size() * sizeof(float));
+    plan.off_zero_rows = off; off = align256(off + plan.zero_rows.size() * sizeof(int32_t));
     plan.off_part_o = off;   off = align256(off + (size_t)n_partial_rows * plan.prm.head_dim * sizeof(float));
     plan.off_part_ml = off;  off = align256(off + (size_t)n_partial_rows * 2 * sizeof(float));
     return off;
@@ -99,13 +102,52 @@ void cut_request(int kv_len, int chunk, int shortest, Cut how, std::vector<int> 
     cuts.push_back(kv_len);
 }
 
-// Decode units when every request is cut into pieces of `chunk` keys.
-int64_t units_of_length(const pod_attn_params &prm, const int32_t *seq_meta, int chunk)
+// Decode units when every request (of so many keys) is cut into pieces of `chunk` keys.
+int64_t units_of_length(const pod_attn_params &prm, const std::vector<int32_t> &keys, int chunk)
 {
     int64_t n = 0;
     for (int r = prm.n_prefill; r < prm.n_prefill + prm.n_decode; ++r)
-        n += (int64_t)prm.n_kv_heads * ceil_div(seq_meta[4 * r + 2], chunk);
+        if (keys[(size_t)r] > 0) n += (int64_t)prm.n_kv_heads * ceil_div(keys[(size_t)r], chunk);
     return n;
+}
+
+// Fills in what a plan keeps of changed scores: each row's interval of visible keys above all.
+pod_status read_scores(const pod_attn_scores &scores, const pod_attn_params &prm, const int32_t *seq_meta, Plan &plan, std::string &err)
+{
+    if (!(scores.logit_cap >= 0.f) || !std::isfinite(scores.logit_cap)) { err = "logit_cap must be finite and not negative"; return POD_ERR_INVALID_ARG; }
+    if (scores.window < 0) { err = "negative window"; return POD_ERR_INVALID_ARG; }
+    const int n_req = prm.n_prefill + prm.n_decode;
+    plan.scored = true;
+    plan.logit_cap = scores.logit_cap;
+    if (scores.slopes) {
+        plan.slopes.assign((size_t)prm.n_q_heads + kMaxGroup, 0.f);
+        for (int h = 0; h < prm.n_q_heads; ++h) {
+            if (!std::isfinite(scores.slopes[h])) { err = fmt("slope of head %lld is not finite", h); return POD_ERR_INVALID_ARG; }
+            plan.slopes[(size_t)h] = scores.slopes[h] * 1.4426950408889634f;
+        }
+    }
+    plan.ranges.assign(2 * ((size_t)plan.n_prefill_rows + (size_t)prm.n_decode), 0);
+    for (int r = 0; r < n_req; ++r) {
+        const int32_t *m = seq_meta + 4 * r;
+        const int64_t row0 = m[0] + (r < prm.n_prefill ? 0 : plan.n_prefill_rows);
+        int prefix = 0;
+        if (scores.prefix_len) {
+            if (scores.prefix_len[r] < 0) { err = fmt("request %lld: negative prefix_len", r); return POD_ERR_INVALID_ARG; }
+            prefix = std::min(scores.prefix_len[r], m[2]);
+        }
+        for (int i = 0; i < m[1]; ++i) {
+            const int pos = m[2] - m[1] + i;
+            int first = scores.window > 0 ? std::max(0, pos - (scores.window - 1)) : 0;
+            if (scores.doc_start) {
+                const int32_t start = scores.doc_start[row0 + i];
+                if (start < 0) { err = fmt("row %lld: negative doc_start", row0 + i); return POD_ERR_INVALID_ARG; }
+                first = std::max(first, start);
+            }
+            plan.ranges[2 * (size_t)(row0 + i)] = first;
+            plan.ranges[2 * (size_t)(row0 + i) + 1] = std::max(pos + 1, prefix);
+        }
+    }
+    return POD_OK;
 }
 
 }  // namespace
@@ -168,7 +210,7 @@ pod_status check_params(const pod_attn_params &prm, std::string &err)
 }
 
 pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n_cus, Plan &plan,
-                      std::string &err)
+                      std::string &err, const pod_attn_scores *scores)
 {
     const pod_status checked = check_params(prm, err);
     if (checked != POD_OK) return checked;
@@ -231,6 +273,32 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
     plan.group = group;
     plan.meta.assign(seq_meta, seq_meta + 4 * (size_t)n_req);
     plan.n_prefill_rows = n_prefill_rows;
+    if (scores) {
+        const pod_status read = read_scores(*scores, prm, seq_meta, plan, err);
+        if (read != POD_OK) return read;
+    }
+    // The keys [first, end) that the rows from token tok0 to tok1 of a request see between them; first == end: none.
+    auto visible = [&](int r, int tok0, int tok1, int &first, int &end) {
+        const int32_t *m = seq_meta + 4 * r;
+        if (!plan.scored) { first = 0; end = m[2] - m[1] + tok1 + 1; return; }
+        const size_t row0 = (size_t)(m[0] + (r < prm.n_prefill ? 0 : n_prefill_rows));
+        first = end = 0;
+        for (int t = tok0; t <= tok1; ++t) {
+            const int32_t *range = plan.ranges.data() + 2 * (row0 + (size_t)t);
+            if (range[0] >= range[1]) continue;
+            first = end == 0 ? range[0] : std::min(first, range[0]);
+            end = std::max(end, range[1]);
+        }
+    };
+    // Keys that each decode request reads, from dfirst (rounded down to a whole step; keys ahead of it are masked) on.
+    std::vector<int32_t> keys((size_t)n_req, 0), dfirst((size_t)n_req, 0);
+    for (int r = prm.n_prefill; r < n_req; ++r) {
+        int first, end;
+        visible(r, 0, 0, first, end);
+        dfirst[(size_t)r] = first;
+        keys[(size_t)r] = first < end ? end - first / kDecodeStep * kDecodeStep : 0;
+        if (first >= end) plan.zero_rows.push_back(seq_meta[4 * r]);
+    }
 
     int64_t next_prow = 0;
 
@@ -238,15 +306,15 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
     int64_t token_heads = 0;
     int longest_decode = 0;
     for (int r = prm.n_prefill; r < n_req; ++r) {
-        token_heads += (int64_t)seq_meta[4 * r + 2] * prm.n_kv_heads;
-        longest_decode = std::max(longest_decode, seq_meta[4 * r + 2]);
+        token_heads += (int64_t)keys[(size_t)r] * prm.n_kv_heads;
+        longest_decode = std::max(longest_decode, keys[(size_t)r]);
     }
     // Keys per streaming wavefront (there are four of those per compute unit).
     const int64_t n_waves = (int64_t)n_cus * kWavesPerWg;
     const int64_t share = (token_heads + n_waves - 1) / n_waves;
     // Does the decode work hold a worker on every compute unit for a good part of the launch?
     const int given_chunk = prm.decode_chunk > 0 ? round_up(prm.decode_chunk, kDecodeStep) : 0;
-    const bool decode_on_every_unit = given_chunk > 0 ? units_of_length(prm, seq_meta, given_chunk) >= n_waves : share >= 512;
+    const bool decode_on_every_unit = given_chunk > 0 ? units_of_length(prm, keys, given_chunk) >= n_waves : share >= 512;
 
     // ---- prefill items -----------------------------------------------------------------
     // Row blocks of 128 packed rows per K/V head; split-KV only when there are too few blocks to
@@ -265,16 +333,21 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         const int s_cap = base_items > 0 ? (int)std::max<int64_t>(1, cap_items / base_items) : 1;
         const int min_split = round_up(prm.prefill_split_len > 0 ? prm.prefill_split_len : 1024, kPrefillKvTile);
         for (int r = 0; r < prm.n_prefill; ++r) {
-            const int q_len = seq_meta[4 * r + 1], kv_len = seq_meta[4 * r + 2];
-            const int prefix = kv_len - q_len;
+            const int q_len = seq_meta[4 * r + 1];
             const int rows_total = q_len * group;
+            std::vector<std::pair<int, int>> seen;                   // keys that each block can see
+            for (int row0 = 0; row0 < rows_total; row0 += kPrefillRows) {
+                int first, end;
+                visible(r, row0 / group, (std::min(row0 + kPrefillRows, rows_total) - 1) / group, first, end);
+                seen.emplace_back(first, end);
+            }
             for (int kvh = 0; kvh < prm.n_kv_heads; ++kvh)
                 for (int row0 = 0; row0 < rows_total; row0 += kPrefillRows) {
                     const int n_rows = std::min(kPrefillRows, rows_total - row0);
-                    const int last_tok = (row0 + n_rows - 1) / group;
-                    const int kmax = prefix + last_tok + 1;          // keys this block can see
-                    const int n_tiles = ceil_div(kmax, kPrefillKvTile);
-                    int s = std::min(s_cap, std::max(1, kmax / min_split));
+                    const int kmin = seen[(size_t)(row0 / kPrefillRows)].first, kmax = seen[(size_t)(row0 / kPrefillRows)].second;
+                    const int base = kmin / kDecodeStep * kDecodeStep;   // tiles begin at a multiple of 16 keys
+                    const int n_tiles = std::max(1, ceil_div(kmax - base, kPrefillKvTile));
+                    int s = std::min(s_cap, std::max(1, (kmax - base) / min_split));
                     const int tps = ceil_div(n_tiles, s);
                     s = ceil_div(n_tiles, tps);
                     int64_t prow_base = -1;
@@ -287,8 +360,8 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
                     for (int i = 0; i < s; ++i) {
                         PrefillItem it;
                         it.req = r; it.kv_head = kvh; it.row0 = row0; it.n_rows = n_rows;
-                        it.kv_begin = i * tps * kPrefillKvTile;
-                        it.kv_end = std::min(kmax, (i + 1) * tps * kPrefillKvTile);
+                        it.kv_begin = std::max(kmin, base + i * tps * kPrefillKvTile);
+                        it.kv_end = std::min(kmax, base + (i + 1) * tps * kPrefillKvTile);
                         it.prow0 = s > 1 ? (int32_t)(prow_base + (int64_t)i * kPrefillRows) : -1;
                         it.split = i;
                         plan.pitems.push_back(it);
@@ -408,7 +481,7 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
             // that a worker's slot gets starts when the worker is done and ends that much later: 512 items of 32K
             // keys beside 4 x 4096 of 4 heads 1128 us whole, 979 cut,
             // beside 16 x 4096 1146 / 976; 64 channels, 2048 + 6144 beside 1 x 3000 216 / 171.
-            const int64_t whole_units = units_of_length(prm, seq_meta, longest_decode);
+            const int64_t whole_units = units_of_length(prm, keys, longest_decode);
             const bool own_slots = n_items + (whole_units + kWavesPerWg - 1) / kWavesPerWg <= (int64_t)kSlotsPerUnit * n_cus;
             if (longest_decode <= worth_merging ||
                 (longest_item > 0 && plan.centries.empty() && longest_decode <= beside_items && whole_units <= waves && own_slots))
@@ -419,7 +492,7 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
                 int lo = 0, hi = limit > shortest ? (int)((limit - shortest + kDecodeStep - 1) / kDecodeStep) : 0;
                 while (lo < hi) {
                     const int mid = (lo + hi) / 2;
-                    if (units_of_length(prm, seq_meta, shortest + mid * kDecodeStep) <= waves) hi = mid;
+                    if (units_of_length(prm, keys, shortest + mid * kDecodeStep) <= waves) hi = mid;
                     else lo = mid + 1;
                 }
                 chunk = shortest + lo * kDecodeStep;
@@ -430,7 +503,7 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
                 // heads per K/V head, the combine kernel still has fewer splits to fetch: items of 2028 keys beside 4 x 1500
                 // 70.4 / 69.9 (16 / 8 heads of 256 channels), 1500 beside 2 x 1500 38.1 / 37.6 (9 / 1 heads of 128).
                 const int piece = round_up(ceil_div(longest_decode, kMergeSplits), kDecodeStep);
-                const int64_t workers = (units_of_length(prm, seq_meta, piece) + kWavesPerWg - 1) / kWavesPerWg;
+                const int64_t workers = (units_of_length(prm, keys, piece) + kWavesPerWg - 1) / kWavesPerWg;
                 if (piece > chunk && plan.centries.empty() && longest_item > 0 && piece <= beside_items / 2 &&
                     n_items + workers <= (int64_t)kSlotsPerUnit * n_cus)
                     chunk = piece;
@@ -462,8 +535,8 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
                 const int whole = chunk + round_up(std::max(chunk / 4, shortest), kDecodeStep) / 2;
                 int64_t whole_token_heads = 0;
                 for (int r = prm.n_prefill; r < n_req; ++r)
-                    if (seq_meta[4 * r + 2] <= whole) whole_token_heads += (int64_t)seq_meta[4 * r + 2] * prm.n_kv_heads;
-                const int64_t n_units = units_of_length(prm, seq_meta, whole), rounds = (n_units + n_waves - 1) / n_waves;
+                    if (keys[(size_t)r] <= whole) whole_token_heads += (int64_t)keys[(size_t)r] * prm.n_kv_heads;
+                const int64_t n_units = units_of_length(prm, keys, whole), rounds = (n_units + n_waves - 1) / n_waves;
                 const int64_t length = (int64_t)longest_decode * std::max(128, prm.head_dim);
                 const int tenths = group <= 2 && length > 128 * 1024 ? 8 : 7;
                 if (2 * whole_token_heads > token_heads && 10 * n_units < tenths * rounds * n_waves && length >= 96 * 1024)
@@ -478,7 +551,8 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
                     size_t n_units = 0, n_rows = merged;
                     int64_t n_partials = next_prow;
                     for (int r = prm.n_prefill; r < n_req; ++r) {
-                        cut_request(seq_meta[4 * r + 2], length, shortest, Cut::kTaper, cuts);
+                        if (keys[(size_t)r] == 0) continue;
+                        cut_request(keys[(size_t)r], length, shortest, Cut::kTaper, cuts);
                         const size_t s = cuts.size() - 1;
                         n_units += s * (size_t)prm.n_kv_heads;
                         if (s > 1) { n_rows += (size_t)prm.n_q_heads; n_partials += (int64_t)s * prm.n_q_heads; }
@@ -495,12 +569,14 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         {
             size_t n_est = 0;
             for (int r = prm.n_prefill; r < n_req; ++r)
-                n_est += (size_t)prm.n_kv_heads * (size_t)(seq_meta[4 * r + 2] / chunk + 5);
+                n_est += (size_t)prm.n_kv_heads * (size_t)(keys[(size_t)r] / chunk + 5);
             plan.dunits.reserve(n_est);
             plan.centries.reserve(plan.centries.size() + (size_t)prm.n_decode * prm.n_kv_heads);
         }
         for (int r = prm.n_prefill; r < n_req; ++r) {
-            cut_request(seq_meta[4 * r + 2], chunk, shortest, how, cuts);
+            if (keys[(size_t)r] == 0) continue;
+            cut_request(keys[(size_t)r], chunk, shortest, how, cuts);
+            const int base = dfirst[(size_t)r] / kDecodeStep * kDecodeStep;
             const int s_eff = (int)cuts.size() - 1;
             for (int kvh = 0; kvh < prm.n_kv_heads; ++kvh) {
                 int64_t prow_base = -1;
@@ -512,8 +588,8 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
                 for (int i = 0; i < s_eff; ++i) {
                     DecodeUnit u;
                     u.req = r; u.kv_head = kvh;
-                    u.t0 = cuts[(size_t)i];
-                    u.t1 = cuts[(size_t)i + 1];
+                    u.t0 = std::max(dfirst[(size_t)r], base + cuts[(size_t)i]);
+                    u.t1 = base + cuts[(size_t)i + 1];
                     u.prow0 = s_eff > 1 ? (int32_t)(prow_base + (int64_t)i * group) : -1;
                     u.split = i; u.q_start = seq_meta[4 * r]; u.cache_row = seq_meta[4 * r + 3];
                     plan.dunits.push_back(u);
@@ -551,7 +627,7 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         // in the units: 8 requests of 400 keys, 32 / 8 heads 9.3 / 8.6, 8 query heads on one K/V head 9.3 / 9.0, 16 of them
         // (64 channels) 9.8 / 10.7; 256 channels with two 14.7 / 14.6, with four 14.8 / 15.1.
         plan.units_merge = group <= kMergeRows && prm.head_dim <= kMergeDim && plan.max_dsplits >= 2 && plan.max_dsplits <= kMergeSplits &&
-                           (int64_t)plan.dunits.size() <= (int64_t)kWavesPerWg * n_cus &&
+                           (int64_t)plan.dunits.size() <= (int64_t)kWavesPerWg * n_cus && !plan.scored &&
                            next_prow - plan.decode_prow0 <= (int64_t)(sizeof(WsHeader::arrived) / sizeof(uint32_t));
         // The first workers to take a decode seat (one per compute unit) start with four fixed
         // units each, the longest ones, and claim nothing for them.  The other units are dealt
@@ -593,8 +669,11 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         int64_t token_row = c.kind == kPrefill ? c.q_start + c.row0 / group : n_prefill_rows + c.q_start;
         int head = c.kind == kPrefill ? c.row0 % group : 0;               // inside the group
         for (int r = 0; r < c.n_rows; ++r) {
+            // (a row that sees nothing is written by its item)
+            const int32_t *range = plan.scored ? plan.ranges.data() + 2 * token_row : nullptr;
+            const bool empty = range && range[0] >= range[1];
             const uint64_t out_row = (uint64_t)(token_row * prm.n_q_heads + c.kv_head * group + head) | decode_bit;
-            plan.merge_rows.push_back(CombineRow{c.prow0 + r, c.n_splits, (uint32_t)out_row, (uint32_t)(out_row >> 32)});
+            if (!empty) plan.merge_rows.push_back(CombineRow{c.prow0 + r, c.n_splits, (uint32_t)out_row, (uint32_t)(out_row >> 32)});
             if (++head == group) { head = 0; ++token_row; }
         }
         if (c.kind == kPrefill) plan.n_crows_prefill = (int)plan.merge_rows.size();
@@ -657,7 +736,7 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         }
         const double flop_time = 4.0 * prm.head_dim * pairs * prm.n_q_heads / 2.5e15;
         const double byte_time = kv_tokens * prm.n_kv_heads * prm.head_dim * 4.0 / 8.0e12;
-        const bool built = built_for_prefill_heavy(prm.block_size, prm.head_dim, prm.n_kv_heads);
+        const bool built = built_for_prefill_heavy(prm.block_size, prm.head_dim, prm.n_kv_heads) && !plan.scored;
         plan.heavy_advised = built && prm.n_prefill > 0 && prm.n_decode > 0 &&
                              flop_time > 1.2 * byte_time;
         // The automatic policy takes that configuration where it was ahead by more than its two streams and three

@@ -31,6 +31,13 @@ struct Plan {
     int n_crows_prefill = 0;                // rows of merge_rows that are prefill rows
     int64_t n_prefill_rows = 0;
     int64_t n_partial_rows = 0;
+    // Plans with changed scores: the interval of visible keys of each row of `out` (first, end), slopes * log2(e) with
+    // kMaxGroup zeros behind them (empty: none), and the decode rows that see nothing.
+    bool scored = false;
+    float logit_cap = 0.f;
+    std::vector<int32_t> ranges;
+    std::vector<float> slopes;
+    std::vector<int32_t> zero_rows;
     int64_t decode_prow0 = 0;               // first partial row of a decode unit
     // Whether the last unit of each decode group merges it (unless the combine kernel has to), and then the number of
     // splits of each unit's group, in the order of `dunits`.
@@ -46,7 +53,7 @@ struct Plan {
     int fixed_roles = kRolesByTicket;       // RoleRule of the fused launch
     int fused_grid = 0;                     // workgroups of the fused kernel
     // byte offsets inside the workspace (each 256-byte aligned)
-    size_t off_pitems = 0, off_pitems_by_wg = 0, off_pitem_of_wg = 0, off_dunits = 0, off_crows = 0, off_dq = 0, off_part_o = 0, off_part_ml = 0;
+    size_t off_pitems = 0, off_pitems_by_wg = 0, off_pitem_of_wg = 0, off_dunits = 0, off_crows = 0, off_dq = 0, off_ranges = 0, off_slopes = 0, off_zero_rows = 0, off_part_o = 0, off_part_ml = 0;
     size_t ws_bytes = 0;
     // events of the two-kernel modes (fork, two joins), created on first use, or with the upload of a plan that
     // takes the prefill-heavy configuration by itself
@@ -62,7 +69,7 @@ struct Plan {
 pod_status check_params(const pod_attn_params &prm, std::string &err);
 // Validates and fills `plan`; returns POD_OK or an error code with a message in `err`.
 pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n_cus, Plan &plan,
-                      std::string &err);
+                      std::string &err, const pod_attn_scores *scores = nullptr);
 
 // Reduce a (prefill workgroups : decode workgroups) count to the small role ratio of Section 4.1.
 void role_ratio(int policy, int n_prefill_wgs, int n_decode_wgs, int &p, int &d);

@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
-from typing import Optional
+from typing import Optional, Sequence
 
 import numpy as np
 
@@ -31,7 +31,7 @@ MODES = {"fused": MODE_FUSED, "serial": MODE_SERIAL, "streams": MODE_STREAMS,
 POLICY_AUTO, POLICY_ALTERNATE, POLICY_PROPORTIONAL = 0, 1, 2
 KV_TOKEN_MAJOR, KV_HEAD_MAJOR = 0, 1
 
-EXPORTS = ["pod_attn_plan_create", "pod_attn_plan_destroy", "pod_attn_plan_info_get",
+EXPORTS = ["pod_attn_plan_create", "pod_attn_plan_create_scored", "pod_attn_plan_destroy", "pod_attn_plan_info_get",
            "pod_attn_workspace_size", "pod_attn_plan_set_trace", "pod_attn_plan_set_event_log",
            "pod_attn_plan_upload", "pod_attn_forward", "pod_attn_forward_static",
            "pod_attn_build_tables", "pod_attn_rope_table", "pod_attn_append",
@@ -70,6 +70,11 @@ class PlanInfo(ctypes.Structure):
                 ("prefill_heavy_chosen", ctypes.c_int32)]
 
 
+class ScoresParams(ctypes.Structure):
+    _fields_ = [("logit_cap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.POINTER(ctypes.c_float)),
+                ("doc_start", ctypes.POINTER(ctypes.c_int32)), ("prefix_len", ctypes.POINTER(ctypes.c_int32))]
+
+
 class RopeParams(ctypes.Structure):
     _fields_ = [("layout", ctypes.c_int32), ("scaling", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
                 ("cos_sin_scale", ctypes.c_float), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
@@ -102,6 +107,8 @@ def lib():
         vp, i32p = ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32)
         L.pod_attn_plan_create.restype = ctypes.c_int
         L.pod_attn_plan_create.argtypes = [ctypes.POINTER(Params), i32p, ctypes.POINTER(vp)]
+        L.pod_attn_plan_create_scored.restype = ctypes.c_int
+        L.pod_attn_plan_create_scored.argtypes = [ctypes.POINTER(Params), ctypes.POINTER(ScoresParams), i32p, ctypes.POINTER(vp)]
         L.pod_attn_plan_destroy.restype = None
         L.pod_attn_plan_destroy.argtypes = [vp]
         L.pod_attn_plan_info_get.restype = ctypes.c_int
@@ -225,6 +232,43 @@ def pod_attn_plan_create(params: Params, seq_meta_host) -> Plan:
     meta, meta_p = _i32(np.asarray(seq_meta_host).reshape(-1, 4))
     handle = ctypes.c_void_p()
     _check(lib().pod_attn_plan_create(ctypes.byref(params), meta_p, ctypes.byref(handle)))
+    return Plan(handle.value, params)
+
+
+@dataclasses.dataclass
+class Scores:
+    """Scores other than plain causal ones (``pod_attn_scores``): capped by ``logit_cap * tanh(s / logit_cap)``, less
+    ``slopes[head]`` times the distance to the key, and masked by a sliding ``window``, by the first key of each row's
+    document (``doc_start``, one per output row) and by prefixes that are seen from everywhere in their request
+    (``prefix_len``, one per request)."""
+    logit_cap: float = 0.0
+    window: int = 0
+    slopes: Optional[Sequence[float]] = None
+    doc_start: Optional[Sequence[int]] = None
+    prefix_len: Optional[Sequence[int]] = None
+
+
+def pod_attn_plan_create_scored(params: Params, scores: Optional[Scores], seq_meta_host) -> Plan:
+    meta, meta_p = _i32(np.asarray(seq_meta_host).reshape(-1, 4))
+    handle = ctypes.c_void_p()
+    if scores is None:
+        _check(lib().pod_attn_plan_create_scored(ctypes.byref(params), None, meta_p, ctypes.byref(handle)))
+        return Plan(handle.value, params)
+    n_rows = int(meta[:params.n_prefill, 1].clip(min=0).sum()) + params.n_decode
+    kept, ptr = [], {}
+    for name, size, dtype, ctype in (("slopes", params.n_q_heads, np.float32, ctypes.c_float),
+                                     ("doc_start", n_rows, np.int32, ctypes.c_int32),
+                                     ("prefix_len", meta.shape[0], np.int32, ctypes.c_int32)):
+        value = getattr(scores, name)
+        if value is None:
+            continue
+        a = np.ascontiguousarray(value, dtype=dtype)
+        if a.shape != (size,):
+            raise ValueError(f"{name} must hold {size} values, not {a.shape}")
+        kept.append(a)
+        ptr[name] = a.ctypes.data_as(ctypes.POINTER(ctype))
+    raw = ScoresParams(scores.logit_cap, scores.window, ptr.get("slopes"), ptr.get("doc_start"), ptr.get("prefix_len"))
+    _check(lib().pod_attn_plan_create_scored(ctypes.byref(params), ctypes.byref(raw), meta_p, ctypes.byref(handle)))
     return Plan(handle.value, params)
 
 
@@ -525,9 +569,10 @@ class TokenAppend:
 
 
 class HybridAttention:
-    """Plan + workspace for one batch shape; ``forward`` may be called once per layer."""
+    """Plan + workspace for one batch shape; ``forward`` may be called once per layer.  ``scores``: scores other than plain
+    causal ones."""
 
-    def __init__(self, batch, *, policy=POLICY_AUTO, max_prefill_waves=0, decode_chunk=0,
+    def __init__(self, batch, *, scores: Optional[Scores] = None, policy=POLICY_AUTO, max_prefill_waves=0, decode_chunk=0,
                  prefill_split_len=0, n_compute_units=0):
         import torch
         self.torch = torch
@@ -541,7 +586,8 @@ class HybridAttention:
             max_prefill_waves=max_prefill_waves, decode_chunk=decode_chunk,
             prefill_split_len=prefill_split_len, n_compute_units=n_compute_units,
             kv_order=KV_HEAD_MAJOR if batch.head_major else KV_TOKEN_MAJOR)
-        self.plan = pod_attn_plan_create(self.params, self.batch_meta)
+        self.plan = (pod_attn_plan_create(self.params, self.batch_meta) if scores is None
+                     else pod_attn_plan_create_scored(self.params, scores, self.batch_meta))
         self.info = self.plan.info()
         dev = batch.k_cache.device
         self.ws_bytes = pod_attn_workspace_size(self.plan)
