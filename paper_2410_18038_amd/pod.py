@@ -438,22 +438,37 @@ def pod_attn_simulate_launch(plan: Plan, unit_of_wg, order):
 # ----------------------------------------------------------------------------------------------
 # Convenience wrapper for torch tensors (marshalling only).
 # ----------------------------------------------------------------------------------------------
-def _on_device(dev):
-    """The device a call's tensors are on has to be the current one."""
+def _stream_of(device) -> int:
+    """The hipStream_t of torch's current stream on a device.  (As an object it costs 1.8 us to ask for, as a number 0.1.)"""
     import torch
-    return torch.cuda.device(dev)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _call(device, function, *args):
+    """function(*args) with `device` as the current one, which is where its tensors are."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        status = function(*args)
+    else:
+        with torch.cuda.device(device):
+            status = function(*args)
+    if status != POD_OK:
+        _check(status)
 
 
 def _need(t, what, dtype, shape, device, strided=False):
-    """Raises ValueError unless t is a tensor of this type and shape on this device, in one piece (with `strided`: whose rows
-    are).  A None in the shape is any size."""
+    """Raises ValueError unless t is a tensor of this type and shape on this device, in one piece (with `strided`, of two
+    dimensions, whose rows are).  A None in the shape is any size."""
+    if t.dtype is dtype and t.shape == shape and t.device == device and (t.stride(1) == 1 if strided else t.is_contiguous()):
+        return
     if t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
     if t.device != device:
         raise ValueError(f"{what} must be on {device}, not {t.device}")
     if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
         raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    if not (t.is_contiguous() or (strided and (t.shape[0] == 0 or t[0].is_contiguous()))):
+    if not (t.is_contiguous() or (strided and t.stride(1) == 1)):
         raise ValueError(f"{what} must lie in one piece" + (" row by row" if strided else ""))
 
 
@@ -499,6 +514,7 @@ class TokenTables:
         self.slots = torch.empty(self.n_rows, dtype=torch.int32, device=self.device)
         self.positions = torch.empty(self.n_rows, dtype=torch.int32, device=self.device)
         self.report = torch.zeros(4, dtype=torch.int32, device=self.device)
+        self._args = ctypes.byref(params), self.n_rows, self.slots.data_ptr(), self.positions.data_ptr(), self.report.data_ptr()
 
     def build(self, seq_meta, free_blocks=None, block_table=None):
         """From seq_meta (int32 [requests, 4]); a paged cache also takes its free blocks and its block table, which is
@@ -511,9 +527,9 @@ class TokenTables:
             _need(free_blocks, "free_blocks", torch.int32, (None,), dev)
             _need(block_table, "block_table", torch.int32, (p.n_cache_rows, p.max_blocks_per_seq), dev)
             free, n_free, table = free_blocks.data_ptr(), free_blocks.numel(), block_table.data_ptr()
-        with _on_device(dev):
-            pod_attn_build_tables(p, seq_meta.data_ptr(), free, n_free, table, self.n_rows, self.slots.data_ptr(),
-                                  self.positions.data_ptr(), self.report.data_ptr(), torch.cuda.current_stream(dev).cuda_stream)
+        ref, n_rows, slots, positions, report = self._args
+        _call(dev, lib().pod_attn_build_tables, ref, seq_meta.data_ptr(), free, n_free, table, n_rows, slots, positions, report,
+              _stream_of(dev))
         return self
 
 
@@ -537,34 +553,34 @@ class TokenAppend:
             self.weights = (norm.q_weight, norm.k_weight)                # kept alive
             ptr = lambda w: None if w is None else w.data_ptr()
             self.norm = HeadNormParams(ptr(norm.q_weight), ptr(norm.k_weight), norm.eps, norm.weight_offset, int(norm.q), int(norm.k))
-
-    def cache_shape(self):
-        p = self.params
-        n, tokens = (p.n_blocks, p.block_size) if p.block_size > 0 else (p.n_cache_rows, p.kv_seq_stride // (p.n_kv_heads * p.head_dim))
-        return (n, p.n_kv_heads, tokens, p.head_dim) if p.kv_order == KV_HEAD_MAJOR else (n, tokens, p.n_kv_heads, p.head_dim)
+        p = params
+        n, tokens = (p.n_blocks, p.block_size) if p.block_size > 0 else (p.n_cache_rows, p.kv_seq_stride // max(p.n_kv_heads * p.head_dim, 1))
+        self.cache_shape = (n, p.n_kv_heads, tokens, p.head_dim) if p.kv_order == KV_HEAD_MAJOR else (n, tokens, p.n_kv_heads, p.head_dim)
+        ref = lambda x: None if x is None else ctypes.byref(x)
+        self._args = ref(params), ref(self.rope), 0 if self.table is None else self.table.data_ptr(), ref(self.norm)
 
     def __call__(self, q, k, v, slots, positions, k_cache, v_cache, q_out=None):
         """q, k, v: [rows, heads * head_dim] (or views of one projection); returns q_out, [rows, Hq, d]."""
         import torch
-        p, dev, rows = self.params, self.device, slots.shape[0]
-        for t, what, heads in ((q, "q", p.n_q_heads), (k, "k", p.n_kv_heads), (v, "v", p.n_kv_heads)):
-            _need(t, what, self.dtype, (rows, heads * p.head_dim), dev, strided=True)
+        p, dev, dtype, rows = self.params, self.device, self.dtype, slots.shape[0]
+        q_row, kv_row = p.n_q_heads * p.head_dim, p.n_kv_heads * p.head_dim
+        _need(q, "q", dtype, (rows, q_row), dev, strided=True)
+        _need(k, "k", dtype, (rows, kv_row), dev, strided=True)
+        _need(v, "v", dtype, (rows, kv_row), dev, strided=True)
         _need(slots, "slots", torch.int32, (rows,), dev)
         _need(positions, "positions", torch.int32, (rows,), dev)
-        for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-            _need(t, what, self.dtype, self.cache_shape(), dev)
+        _need(k_cache, "k_cache", dtype, self.cache_shape, dev)
+        _need(v_cache, "v_cache", dtype, self.cache_shape, dev)
         if q_out is None:
-            q_out = torch.empty((rows, p.n_q_heads, p.head_dim), dtype=self.dtype, device=dev)
+            q_out = torch.empty((rows, p.n_q_heads, p.head_dim), dtype=dtype, device=dev)
         else:
-            _need(q_out, "q_out", self.dtype, (rows, p.n_q_heads, p.head_dim), dev)
-        if rows == 0:
-            return q_out
-        stride = lambda t: t.stride(0) if rows > 1 else t.shape[1]
-        with _on_device(dev):
-            pod_attn_append(p, self.rope, 0 if self.table is None else self.table.data_ptr(), self.norm, q.data_ptr(), stride(q),
-                            k.data_ptr(), stride(k), v.data_ptr(), stride(v), slots.data_ptr(), positions.data_ptr(), rows,
-                            q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                            torch.cuda.current_stream(dev).cuda_stream)
+            _need(q_out, "q_out", dtype, (rows, p.n_q_heads, p.head_dim), dev)
+        # (a single row has no distance to a next one: torch may name any)
+        q_stride, k_stride, v_stride = (q.stride(0), k.stride(0), v.stride(0)) if rows > 1 else (q_row, kv_row, kv_row)
+        ref, rope, table, norm = self._args
+        _call(dev, lib().pod_attn_append, ref, rope, table, norm, q.data_ptr(), q_stride, k.data_ptr(), k_stride, v.data_ptr(),
+              v_stride, slots.data_ptr(), positions.data_ptr(), rows, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+              _stream_of(dev))
         return q_out
 
 
@@ -605,10 +621,9 @@ class HybridAttention:
             out = torch.empty((batch.n_rows, batch.n_q_heads, batch.head_dim), dtype=batch.torch_dtype,
                               device=dev)
         ptr = lambda t: 0 if t is None or t.numel() == 0 else t.data_ptr()
-        stream = torch.cuda.current_stream(dev).cuda_stream
-        pod_attn_forward(ptr(batch.prefill_q), ptr(batch.decode_q), ptr(batch.k_cache), ptr(batch.v_cache),
-                         self.seq_meta_dev.data_ptr(), ptr(batch.block_table), out.data_ptr(), self.plan,
-                         self.ws_ptr, self.ws_bytes, mode, stream)
+        _call(dev, lib().pod_attn_forward, ptr(batch.prefill_q), ptr(batch.decode_q), ptr(batch.k_cache), ptr(batch.v_cache),
+              self.seq_meta_dev.data_ptr(), ptr(batch.block_table), out.data_ptr(), self.plan.handle, self.ws_ptr, self.ws_bytes,
+              mode, _stream_of(dev))
         return out
 
     def forward_tokens(self, batch, append: TokenAppend, tables: TokenTables, q, k, v, out=None, mode=MODE_FUSED):
