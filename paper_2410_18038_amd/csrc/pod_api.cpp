@@ -776,11 +776,7 @@ pod_status pod_attn_append(const pod_attn_params *params, const pod_rope_params 
     a.tok_stride = (int32_t)(head_major ? d : hkv * d);
     a.head_stride = head_major ? (int64_t)a.per_block * d : d;
     a.n_rows = n_rows; a.n_q_heads = prm.n_q_heads; a.n_kv_heads = prm.n_kv_heads;
-    const int heads = pod::append_heads(prm.head_dim);
-    const int n_steps = (prm.n_q_heads + 2 * prm.n_kv_heads + heads - 1) / heads;
-    a.steps_per_wave = n_steps;
-    const int parts = (n_steps + a.steps_per_wave - 1) / a.steps_per_wave;
-    const hipError_t e = pod::launch_append(a, prm.dtype, prm.head_dim, layout, parts, (hipStream_t)stream);
+    const hipError_t e = pod::launch_append(a, prm.dtype, prm.head_dim, layout, (hipStream_t)stream);
     return e == hipSuccess ? POD_OK : fail_hip(e, "launching the append kernel");
 }
 

@@ -41,11 +41,10 @@ struct AppendArgs {
     int32_t rot_dim;                       // 0: no rotation
     float cos_sin_scale, eps, weight_offset;
     int32_t norm_q, norm_k;
-    int32_t steps_per_wave;                // groups of heads that one wavefront does one after the other
 };
 
 hipError_t launch_tables(const TableArgs &a, hipStream_t stream);
-hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, int layout, int parts, hipStream_t stream);
+hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, int layout, hipStream_t stream);
 // Heads that a wavefront of the append kernel works on at a time.
 constexpr int append_heads(int head_dim) { return kWaveSize * 16 / head_dim; }
 

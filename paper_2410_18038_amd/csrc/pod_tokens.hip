@@ -146,61 +146,79 @@ hipError_t launch_tables(const TableArgs &a, hipStream_t stream)
 // its own: pieces p and p + rot_dim / 16 with the half layout, neighbours with the interleaved one and behind the rotated
 // channels.  Normalising a head is then a sum over head_dim / 16 neighbouring lanes and rotating it needs no exchange.
 // A wavefront works on one row, 1024 / head_dim heads at a time, query, key and value heads alike; a lane's pairs are the
-// same in every head, so that their cosines and sines are worked out once a row.  The angle is a fixed-point product: the
+// same in every head, and their cosines and sines are worked out once a row and group of heads.  The angle is a fixed-point product: the
 // pair's turns per position as a fraction of 2^64 times the position, whose upper word is the angle as a signed fraction
 // of a turn to 2^-32, for every position; the sine unit takes turns.
+// What bounds it is memory for many rows (8192 rows, 32 / 8 heads of 128 channels, 201 MB: 33 us, 6.1 TB/s, the inputs
+// partly in the last-level cache; 8192 x 32 / 32 heads, 403 MB: 79 us, 5.1 TB/s) and the launch for few (16 rows 3.0 us).
+// 54 and 11.8 us with one wavefront a row, angles worked out by every lane and the loads behind the slot's.
 // ------------------------------------------------------------------------------------------
 template <int DT> struct Elem;
 template <> struct Elem<0> { using t = _Float16; };
 template <> struct Elem<1> { using t = __bf16; };
 
-template <int DT, int D, int ROPE>
+template <int DT, int D, int ROPE, int STEPS>
 __global__ __launch_bounds__(kWgThreads) void append_tokens(AppendArgs a)
 {
     using elem = typename Elem<DT>::t;
     typedef elem e8 __attribute__((ext_vector_type(8)));
     constexpr int LPH = D / 16, HPW = kWaveSize / LPH;
-    const int lane = threadIdx.x & 63;
-    const int row = (int)blockIdx.x * kWavesPerWg + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ __attribute__((aligned(16))) float turn[kWavesPerWg][D];      // cosine and sine of each pair of a row
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = (int)blockIdx.x * kWavesPerWg + wave;
     if (row >= a.n_rows) return;
     const int slot = ((const POD_CONST int32_t *)a.slots)[row], pos = ((const POD_CONST int32_t *)a.positions)[row];
-    if (slot < 0 || slot >= a.n_slots) return;
-    int at;
-    const int block = divide(slot, a.per_block, a.magic, at);
-    const int64_t cache_base = (int64_t)block * a.block_elems + (int64_t)at * a.tok_stride;
     const int sub = lane % LPH, pairs = a.rot_dim / 16;
     const bool turns = sub < pairs;
     int c0 = 2 * sub, c1 = 2 * sub + 1;               // the lane's pieces of a head
     if (ROPE == POD_ROPE_HALF && turns) { c0 = sub; c1 = sub + pairs; }
+    // The heads are asked for ahead of what they wait for, of padding rows as well.
+    const int n_heads = a.n_q_heads + 2 * a.n_kv_heads;
+    const int head0 = (int)blockIdx.y * STEPS * HPW + lane / LPH;
+    e8 in[STEPS][2];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int head = min(head0 + s * HPW, n_heads - 1), k = head - a.n_q_heads, v = k - a.n_kv_heads;
+        const elem *src = k < 0 ? (const elem *)a.q + row * a.q_stride + head * D
+                                : (v < 0 ? (const elem *)a.k + row * a.k_stride + k * D : (const elem *)a.v + row * a.v_stride + v * D);
+        in[s][0] = *(const e8 *)(src + c0 * 8);
+        in[s][1] = *(const e8 *)(src + c1 * 8);
+    }
+    if (slot < 0 || slot >= a.n_slots) return;
+    int at;
+    const int block = divide(slot, a.per_block, a.magic, at);
+    const int64_t cache_base = (int64_t)block * a.block_elems + (int64_t)at * a.tok_stride;
+    // A pair's cosine and sine are worked out by one lane (or two pairs by it) and handed to the lanes of all heads through
+    // LDS: worked out by every lane for itself they were half of the kernel's vector work.
     float cs[8], sn[8];
-    if (turns) {
-        const uint64_t *f = a.table + 8 * sub;
+    if (pairs > 0) {
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const u32x4 w = *(const u32x4 *)(f + i);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t angle = __umulhi((uint32_t)pos, w[2 * j]) + (uint32_t)pos * w[2 * j + 1];
-                if (pos < 0) angle -= w[2 * j];
+        for (int i = lane; i < D / 2; i += kWaveSize)
+            if (i < 8 * pairs) {
+                const u32x2 f = *(const u32x2 *)(a.table + i);
+                uint32_t angle = __umulhi((uint32_t)pos, f[0]) + (uint32_t)pos * f[1];
+                if (pos < 0) angle -= f[0];
                 const float x = (float)(int32_t)angle * 0x1p-32f;
-                cs[i + j] = __builtin_amdgcn_cosf(x) * a.cos_sin_scale;
-                sn[i + j] = __builtin_amdgcn_sinf(x) * a.cos_sin_scale;
+                turn[wave][2 * i] = __builtin_amdgcn_cosf(x) * a.cos_sin_scale;
+                turn[wave][2 * i + 1] = __builtin_amdgcn_sinf(x) * a.cos_sin_scale;
             }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        if (turns) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { cs[i] = turn[wave][16 * sub + 2 * i]; sn[i] = turn[wave][16 * sub + 2 * i + 1]; }
         }
     }
-    const int n_heads = a.n_q_heads + 2 * a.n_kv_heads;
-    const int n_steps = (n_heads + HPW - 1) / HPW;
-    const int s0 = (int)blockIdx.y * a.steps_per_wave, s1 = min(n_steps, s0 + a.steps_per_wave);
-    for (int s = s0; s < s1; ++s) {
-        const int head = s * HPW + lane / LPH;
-        if (head >= n_heads) continue;                // (whole groups of lanes; the last step alone)
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int head = head0 + s * HPW;
+        if (head >= n_heads) break;                   // (whole groups of lanes)
         const bool is_q = head < a.n_q_heads, is_k = !is_q && head < a.n_q_heads + a.n_kv_heads;
         const int kv = head - a.n_q_heads - (is_k ? 0 : a.n_kv_heads);
-        const elem *src = is_q ? (const elem *)a.q + row * a.q_stride + head * D
-                               : (is_k ? (const elem *)a.k + row * a.k_stride : (const elem *)a.v + row * a.v_stride) + kv * D;
         elem *dst = is_q ? (elem *)a.q_out + ((int64_t)row * a.n_q_heads + head) * D
                          : (elem *)(is_k ? a.k_cache : a.v_cache) + cache_base + kv * a.head_stride;
-        e8 r0 = *(const e8 *)(src + c0 * 8), r1 = *(const e8 *)(src + c1 * 8);
+        e8 r0 = in[s][0], r1 = in[s][1];
         const bool norm = is_q ? a.norm_q : is_k && a.norm_k;
         float x[8], y[8];
 #pragma unroll
@@ -212,13 +230,17 @@ __global__ __launch_bounds__(kWgThreads) void append_tokens(AppendArgs a)
 #pragma unroll
             for (int d = 1; d < LPH; d *= 2) ss += __shfl_xor(ss, d);
             const float inv = rsqrtf(ss * (1.f / D) + a.eps);
-            if (norm) {
-                const elem *w = (const elem *)(is_q ? a.q_weight : a.k_weight);
+            const elem *w = (const elem *)(is_q ? a.q_weight : a.k_weight);
+            if (norm && w) {
+                const e8 w0 = *(const e8 *)(w + c0 * 8), w1 = *(const e8 *)(w + c1 * 8);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x[i] *= inv * (w ? (float)w[c0 * 8 + i] + a.weight_offset : 1.f);
-                    y[i] *= inv * (w ? (float)w[c1 * 8 + i] + a.weight_offset : 1.f);
+                    x[i] *= inv * ((float)w0[i] + a.weight_offset);
+                    y[i] *= inv * ((float)w1[i] + a.weight_offset);
                 }
+            } else if (norm) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { x[i] *= inv; y[i] *= inv; }
             }
         }
         const bool turned = turns && (is_q || is_k);
@@ -251,23 +273,35 @@ __global__ __launch_bounds__(kWgThreads) void append_tokens(AppendArgs a)
     }
 }
 
-template <int DT, int D>
-static hipError_t launch_append_as(const AppendArgs &a, int layout, int parts, hipStream_t stream)
+template <int DT, int D, int STEPS>
+static hipError_t launch_append_steps(const AppendArgs &a, int layout, hipStream_t stream)
 {
-    const dim3 grid((a.n_rows + kWavesPerWg - 1) / kWavesPerWg, parts), threads(kWgThreads);
-    if (layout == POD_ROPE_HALF) append_tokens<DT, D, POD_ROPE_HALF><<<grid, threads, 0, stream>>>(a);
-    else append_tokens<DT, D, POD_ROPE_INTERLEAVED><<<grid, threads, 0, stream>>>(a);
+    constexpr int heads = append_heads(D) * STEPS;
+    const int n_heads = a.n_q_heads + 2 * a.n_kv_heads;
+    const dim3 grid((a.n_rows + kWavesPerWg - 1) / kWavesPerWg, (n_heads + heads - 1) / heads), threads(kWgThreads);
+    if (layout == POD_ROPE_HALF) append_tokens<DT, D, POD_ROPE_HALF, STEPS><<<grid, threads, 0, stream>>>(a);
+    else append_tokens<DT, D, POD_ROPE_INTERLEAVED, STEPS><<<grid, threads, 0, stream>>>(a);
     return hipGetLastError();
 }
-
-hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, int layout, int parts, hipStream_t stream)
+template <int DT, int D>
+static hipError_t launch_append_as(const AppendArgs &a, int layout, hipStream_t stream)
 {
-    if (dtype == POD_F16 && head_dim == 64) return launch_append_as<0, 64>(a, layout, parts, stream);
-    if (dtype == POD_F16 && head_dim == 128) return launch_append_as<0, 128>(a, layout, parts, stream);
-    if (dtype == POD_F16 && head_dim == 256) return launch_append_as<0, 256>(a, layout, parts, stream);
-    if (dtype == POD_BF16 && head_dim == 64) return launch_append_as<1, 64>(a, layout, parts, stream);
-    if (dtype == POD_BF16 && head_dim == 128) return launch_append_as<1, 128>(a, layout, parts, stream);
-    if (dtype == POD_BF16 && head_dim == 256) return launch_append_as<1, 256>(a, layout, parts, stream);
+    // One group of heads a wavefront up to a few rounds of the chip, then two, which halves the work on angles.  us at 128
+    // channels, 32 / 8 heads, one group / two / four: 16 rows 3.0 / 3.6 / 5.0, 256 rows 3.5 / 4.0 / 5.4, 1024 rows (6144
+    // wavefronts of one group) 6.2 / 6.1 / 7.0; 256 channels, 4096 rows 26.6 / 23.4 / 25.1; 64 channels, 1024 rows (3072)
+    // 4.30 / 4.33 / 5.1, 2048 rows 6.1 / 5.9.
+    const int64_t waves = (int64_t)a.n_rows * ((a.n_q_heads + 2 * a.n_kv_heads + append_heads(D) - 1) / append_heads(D));
+    return waves < 6 * 1024 ? launch_append_steps<DT, D, 1>(a, layout, stream) : launch_append_steps<DT, D, 2>(a, layout, stream);
+}
+
+hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, int layout, hipStream_t stream)
+{
+    if (dtype == POD_F16 && head_dim == 64) return launch_append_as<0, 64>(a, layout, stream);
+    if (dtype == POD_F16 && head_dim == 128) return launch_append_as<0, 128>(a, layout, stream);
+    if (dtype == POD_F16 && head_dim == 256) return launch_append_as<0, 256>(a, layout, stream);
+    if (dtype == POD_BF16 && head_dim == 64) return launch_append_as<1, 64>(a, layout, stream);
+    if (dtype == POD_BF16 && head_dim == 128) return launch_append_as<1, 128>(a, layout, stream);
+    if (dtype == POD_BF16 && head_dim == 256) return launch_append_as<1, 256>(a, layout, stream);
     return hipErrorInvalidValue;
 }
 
