@@ -136,7 +136,19 @@ pod::ScoredArgs make_scored(const pod::Plan &p, const pod::KernelArgs &a, const 
     s.zero_rows = (const int32_t *)(ws + p.off_zero_rows);
     s.n_zero_rows = (int32_t)p.zero_rows.size();
     s.cap_log2 = p.logit_cap * 1.4426950408889634f;
-    s.cap_exp = p.logit_cap > 0.f ? 2.f * 1.4426950408889634f * p.prm.softmax_scale / p.logit_cap : 0.f;
+    s.cap_exp = s.cap_limit = 0.f;
+    for (float &c : s.cap_poly) c = 0.f;
+    if (p.logit_cap > 0.f) {
+        // tanh y = y (a0 + a1 y^2 + ...) with y = k s
+        const double k = (double)p.prm.softmax_scale / p.logit_cap, fit[4] = {0.999999456, -0.33326318, 0.131902967, -0.0444022262};
+        double power = 1.4426950408889634 * p.logit_cap * k;
+        s.cap_exp = (float)(2.0 * 1.4426950408889634 * k);
+        for (int i = 0; i < 4; ++i, power *= k * k) s.cap_poly[i] = (float)(power * fit[i]);
+        // Coefficients that leave the range of 32 bits: for caps far above the scores only |y| <= 1/50, where the upper two
+        // do not count; for caps far below them the polynomial is not used.
+        const double last = std::fabs(power / (k * k) * fit[3]);
+        s.cap_limit = (float)((last < 1e-30 ? 0.02 : last > 1e30 ? 0.0 : 0.5) / k);
+    }
     return s;
 }
 

@@ -221,6 +221,8 @@ struct ScoredArgs : KernelArgs {
     const int32_t *zero_rows;              // decode rows that see no key
     int32_t n_zero_rows;
     float cap_exp;                         // 2 * log2(e) * softmax_scale / logit_cap
+    float cap_limit;                       // the polynomial holds for dot products up to this,
+    float cap_poly[4];                     // and is s * (cap_poly[0] + cap_poly[1] s^2 + ...)
 };
 
 }  // namespace pod

@@ -228,41 +228,72 @@ __device__ __forceinline__ int wave_min32(int x)
     return __builtin_amdgcn_readfirstlane(x);
 }
 
-// What a score is multiplied by to be in units of log2(e) (1 where change_scores has done that).
+// What a score (the dot product, with its bias, or a capped one) is multiplied by to be in units of log2(e).
 __device__ __forceinline__ float score_unit(const KernelArgs &a) { return a.scale_log2; }
-__device__ __forceinline__ float score_unit(const ScoredArgs &a) { return a.cap_log2 != 0.f || a.slopes ? 1.f : a.scale_log2; }
+__device__ __forceinline__ float score_unit(const ScoredArgs &a) { return a.cap_log2 != 0.f ? 1.f : a.scale_log2; }
 
-// Score of one key in units of log2(e) from its dot product: cap * tanh(s / cap), with tanh y = 1 - 2 / (1 + e^2y).
-// (Where e^2y overflows or vanishes that is 1 or -1.)  The result is off by 2^-22 of the cap at the most.
-__device__ __forceinline__ float capped(const ScoredArgs &a, float s)
+// Caps scores: from dot products to cap * tanh(s / cap) in units of log2(e).  Where all scores of the wavefront are below
+// half of the cap, which is what a cap is for, s times a polynomial in s^2 (within 2^-20.8 of the score: the relative
+// minimax fit of tanh y / y with four terms on |y| <= 1/2); otherwise 1 - 2 / (1 + e^2y), which is within 2^-22 of the cap,
+// where e^2y overflows or vanishes as well.  An element is five instructions, or seven with two of a quarter rate: prefill
+// of 2048 tokens at 32K, 32 / 4 heads of 128 channels, POLY / EXP us.
+template <class V, int NB>
+__device__ __forceinline__ void cap_scores(const ScoredArgs &a, V (&s)[NB])
 {
-    const float e = fast_exp2(s * a.cap_exp);
-    return __builtin_fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(1.f + e), a.cap_log2);
+    constexpr int E = sizeof(V) / sizeof(float);
+    float top = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < E; ++r) top = fmaxf(top, fabsf(s[b][r]));
+    if (__builtin_amdgcn_ballot_w64(top > a.cap_limit) == 0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < E; ++r) {
+                const float x = s[b][r], t = x * x;
+                s[b][r] = x * __builtin_fmaf(t, __builtin_fmaf(t, __builtin_fmaf(t, a.cap_poly[3], a.cap_poly[2]), a.cap_poly[1]), a.cap_poly[0]);
+            }
+    } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < E; ++r) {
+                const float e = fast_exp2(s[b][r] * a.cap_exp);
+                s[b][r] = __builtin_fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(1.f + e), a.cap_log2);
+            }
+    }
 }
 
-// The scores of a tile in units of log2(e), from the dot products, where they are capped or fall with distance; `ahead` is
-// the distance from the row's own token to the lane's first key.
+// The bias of a capped tile's scores: `ahead` is the distance from the row's own token to the lane's first key.
 template <int NTB>
-__device__ __forceinline__ void change_scores(const ScoredArgs &a, f32x16 (&s)[NTB], float slope, int ahead)
+__device__ __forceinline__ void add_bias(f32x16 (&s)[NTB], float slope, int ahead)
 {
-    if (a.cap_log2 != 0.f) {
+    const float base = (float)ahead;
+#pragma unroll
+    for (int tb = 0; tb < NTB; ++tb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            s[tb][r] = __builtin_fmaf(-slope, fabsf(base + (float)(tb * 32 + 8 * (r >> 2) + (r & 3))), s[tb][r]);
+}
+
+// Without a cap the bias is what a tile's products are added to.  For a tile that lies before all rows' own tokens the
+// distance has one sign and the bias of a register is one multiply-add.
+template <int NTB>
+__device__ __forceinline__ void start_from_bias(f32x16 (&s)[NTB], float slope, int ahead, bool one_sign)
+{
+    const float base = (float)ahead;
+    if (one_sign) {
+        const float from = slope * base;
 #pragma unroll
         for (int tb = 0; tb < NTB; ++tb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[tb][r] = capped(a, s[tb][r]);
-    } else if (a.slopes) {
+            for (int r = 0; r < 16; ++r) s[tb][r] = __builtin_fmaf(slope, (float)(tb * 32 + 8 * (r >> 2) + (r & 3)), from);
+    } else {
 #pragma unroll
         for (int tb = 0; tb < NTB; ++tb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[tb][r] *= a.scale_log2;
-    }
-    if (a.slopes) {
-        const float base = (float)ahead;
-#pragma unroll
-        for (int tb = 0; tb < NTB; ++tb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[tb][r] = __builtin_fmaf(-slope, fabsf(base + (float)(tb * 32 + 8 * (r >> 2) + (r & 3))), s[tb][r]);
+            for (int r = 0; r < 16; ++r) s[tb][r] = -slope * fabsf(base + (float)(tb * 32 + 8 * (r >> 2) + (r & 3)));
     }
 }
 
@@ -355,16 +386,16 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
     int wave_maxpos = wave_has_rows ? prefix + w_last / group : -1;
     // Changed scores: the row's first visible key, the wavefront's bounds of those, the slope of the row's head.  Rows that
     // see nothing do not take part in the bounds, and get their zeros here, from the first of the items that share the row.
-    int first = 0, wave_minfirst = 0, wave_maxfirst = 0;
+    int first = 0, wave_minfirst = 0, wave_maxfirst = 0, wave_minown = 0;
     float slope = 0.f;
-    const int key_of_row = row_ok ? prefix + tok : 0;      // where the row's own token sits
+    const int key_of_row = prefix + min(tok, q_len - 1);   // where the row's own token sits
     if constexpr (SCORED) {
         int last = -1;
         if (row_ok) {
             const int32_t *range = a.ranges + 2 * (int64_t)(q_start + tok);
             first = range[0];
             last = range[1] - 1;
-            if (a.slopes) slope = a.slopes[hq];
+            if (a.slopes) slope = a.slopes[hq] * (a.cap_log2 != 0.f ? 1.f : 1.f / a.scale_log2);
         }
         if (row_ok && first > last && it.split == 0) {
             typename N::elem *op = (typename N::elem *)a.out + ((int64_t)(q_start + tok) * a.n_q_heads + hq) * D;
@@ -376,6 +407,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
         row_ok = first <= last;
         pos = row_ok ? last : 0x7fffffff;
         if (!row_ok) first = 0;
+        wave_minown = wave_min32(key_of_row);
         wave_minpos = wave_min32(row_ok ? last : 0x7fffffff);
         wave_maxpos = -wave_min32(row_ok ? -last : 1);
         wave_minfirst = wave_min32(row_ok ? first : 0x7fffffff);
@@ -586,7 +618,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
 
     // S^T = K Q^T for one tile: rows = keys, columns = this wavefront's query rows.
     // Register r of block tb holds key j0 + tb*32 + 8*(r/4) + 4*h + r%4.
-    auto scores = [&](int kbuf, f32x16 (&s)[NTB]) {
+    auto scores = [&](int kbuf, f32x16 (&s)[NTB], [[maybe_unused]] int j0) {
         const POD_LDS unsigned char *kb = lds + kbuf * L::kTileBytes;
         uint32_t k_base = k_rd0;
         asm("" : "+v"(k_base));                   // opaque copy: the XORs below stay inside the loop
@@ -605,6 +637,8 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
         for (int tb = 0; tb < NTB; ++tb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[tb][r] = 0.f;
+        if constexpr (SCORED)
+            if (a.slopes && a.cap_log2 == 0.f) start_from_bias(s, slope, j0 + 4 * h - key_of_row, j0 + T <= wave_minown);
 #pragma unroll
         for (int i = 0; i < kOps; ++i) {
             if (i + kAhead < kOps) kk[i + kAhead] = k_frag(i + kAhead);
@@ -649,7 +683,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
     // and odd tiles) so that the swap is a matter of names, not of 32 register moves per tile, and
     // the LDS buffer of a tile is known at compile time.
     f32x16 s_even[NTB], s_odd[NTB];
-    if (kv_base <= wave_maxpos && (!SCORED || kv_base + T > wave_minfirst)) scores(0, s_even);
+    if (kv_base <= wave_maxpos && (!SCORED || kv_base + T > wave_minfirst)) scores(0, s_even, kv_base);
     __syncthreads();                                         // K tile 0 is free to be overwritten
 
     auto tile_step = [&](const int jt, auto parity, f32x16 (&s_cur)[NTB], f32x16 (&s_next)[NTB])
@@ -682,14 +716,17 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
         // Matrix blocks ask for issue before the other wavefront's softmax: the two then settle into
         // opposite phases.  (At 256 channels raised priority costs the decode stream more; see the worker.)
         if constexpr (D <= 128) __builtin_amdgcn_s_setprio(3);
-        if (next_live) scores(cur ^ 1, s_next);              // matrix unit: scores of the next tile
+        if (next_live) scores(cur ^ 1, s_next, j0 + T);              // matrix unit: scores of the next tile
         if constexpr (D <= 128) __builtin_amdgcn_s_setprio(2);
         if (live) {
             // vector ALUs: softmax of the current tile
             bool need_mask = (j0 + T - 1 > wave_minpos) || (j0 + T > it.kv_end);
             if constexpr (SCORED) {
                 need_mask = need_mask || j0 < wave_maxfirst;
-                change_scores(a, s_cur, slope, j0 + 4 * h - key_of_row);
+                if (a.cap_log2 != 0.f) {
+                    cap_scores(a, s_cur);
+                    if (a.slopes) add_bias(s_cur, slope, j0 + 4 * h - key_of_row);
+                }
             }
             if (__builtin_expect(need_mask, 0)) {
                 const int lim = min(pos, it.kv_end - 1);
@@ -812,8 +849,11 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
                 __syncthreads();
                 if (j0 > wave_maxpos || j0 + T <= wave_minfirst) continue;
                 f32x16 s[NTB];
-                scores(0, s);
-                change_scores(a, s, slope, j0 + 4 * h - key_of_row);
+                scores(0, s, j0);
+                if (a.cap_log2 != 0.f) {
+                    cap_scores(a, s);
+                    if (a.slopes) add_bias(s, slope, j0 + 4 * h - key_of_row);
+                }
                 float mx = neg_inf();
 #pragma unroll
                 for (int tb = 0; tb < NTB; ++tb)
@@ -1377,7 +1417,7 @@ __device__ __forceinline__ int decode_worker_run(const A &a, unsigned char *smem
                 float x = 0.f;
 #pragma unroll
                 for (int g = 0; g < kMaxGroup; ++g) x = n16 == g ? sl[g] : x;    // (kMaxGroup more are there than heads)
-                slope = x;
+                slope = x * (a.cap_log2 != 0.f ? 1.f : 1.f / a.scale_log2);
                 key_of_row = ((const POD_CONST int32_t *)a.seq_meta)[4 * d.req + 2] - 1;
             }
         }
@@ -1409,11 +1449,14 @@ __device__ __forceinline__ int decode_worker_run(const A &a, unsigned char *smem
         const int n_valid = min(cu.t1 - t_first, STEP) - 4 * b4;         // keys of this lane that exist
         if constexpr (SCORED) {
             const int n_ahead = cu.t0 - t_first - 4 * b4;                // ... of which these are ahead of the unit's first key
+            if (a.cap_log2 != 0.f) {
+                f32x4 one[1] = {s};
+                cap_scores(a, one);
+                s = one[0];
+            }
             const float base = (float)(t_first + 4 * b4 - key_of_row);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (a.cap_log2 != 0.f) s[r] = capped(a, s[r]);
-                else if (a.slopes) s[r] *= a.scale_log2;
                 if (a.slopes) s[r] = __builtin_fmaf(-slope, fabsf(base + (float)r), s[r]);
                 s[r] = (r >= n_ahead) ? s[r] : neg_inf();
             }
