@@ -11,10 +11,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpod_attn.so")
 SOURCES = ["pod_kernels.hip", "pod_probe.hip", "pod_tokens.hip", "pod_planner.cpp", "pod_api.cpp"]
-# (source, extra flags) of every object: the kernels are compiled twice per 16-bit type and head_dim, as they are and with
-# changed scores
+# (source, extra flags) of every object: the kernels are compiled three times per 16-bit type and head_dim, as they are, with
+# changed scores and with capped ones
 UNITS = ([("pod_kernels.hip", (f"-DPOD_INSTANCE_DT={dt}", f"-DPOD_INSTANCE_D={d}", *scored))
-          for scored in (("-DPOD_INSTANCE_SCORED",), ()) for dt in (0, 1) for d in (128, 256, 64)]
+          for scored in (("-DPOD_INSTANCE_SCORED=CappedArgs",), ("-DPOD_INSTANCE_SCORED=ScoredArgs",), ()) for dt in (0, 1) for d in (128, 256, 64)]
          + [(src, ()) for src in SOURCES])
 HEADERS = ["pod_common.h", "pod_launch.h", "pod_planner.h", "pod_tokens.h", os.path.join("..", "..", "include", "pod_attn.h")]
 # Packed-fp32 instructions are switched off for the device pass (the host pass does not know

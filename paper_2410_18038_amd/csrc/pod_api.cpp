@@ -135,20 +135,23 @@ pod::ScoredArgs make_scored(const pod::Plan &p, const pod::KernelArgs &a, const 
     s.slopes = p.slopes.empty() ? nullptr : (const float *)(ws + p.off_slopes);
     s.zero_rows = (const int32_t *)(ws + p.off_zero_rows);
     s.n_zero_rows = (int32_t)p.zero_rows.size();
+    return s;
+}
+
+pod::CappedArgs make_capped(const pod::Plan &p, const pod::ScoredArgs &a)
+{
+    pod::CappedArgs s;
+    static_cast<pod::ScoredArgs &>(s) = a;
+    // tanh y = y (a0 + a1 y^2 + ...) with y = k s
+    const double k = (double)p.prm.softmax_scale / p.logit_cap, fit[4] = {0.999999456, -0.33326318, 0.131902967, -0.0444022262};
+    double power = 1.4426950408889634 * p.logit_cap * k;
     s.cap_log2 = p.logit_cap * 1.4426950408889634f;
-    s.cap_exp = s.cap_limit = 0.f;
-    for (float &c : s.cap_poly) c = 0.f;
-    if (p.logit_cap > 0.f) {
-        // tanh y = y (a0 + a1 y^2 + ...) with y = k s
-        const double k = (double)p.prm.softmax_scale / p.logit_cap, fit[4] = {0.999999456, -0.33326318, 0.131902967, -0.0444022262};
-        double power = 1.4426950408889634 * p.logit_cap * k;
-        s.cap_exp = (float)(2.0 * 1.4426950408889634 * k);
-        for (int i = 0; i < 4; ++i, power *= k * k) s.cap_poly[i] = (float)(power * fit[i]);
-        // Coefficients that leave the range of 32 bits: for caps far above the scores only |y| <= 1/50, where the upper two
-        // do not count; for caps far below them the polynomial is not used.
-        const double last = std::fabs(power / (k * k) * fit[3]);
-        s.cap_limit = (float)((last < 1e-30 ? 0.02 : last > 1e30 ? 0.0 : 0.5) / k);
-    }
+    s.cap_exp = (float)(2.0 * 1.4426950408889634 * k);
+    for (int i = 0; i < 4; ++i, power *= k * k) s.cap_poly[i] = (float)(power * fit[i]);
+    // Coefficients that leave the range of 32 bits: for caps far above the scores only |y| <= 1/50, where the upper two do
+    // not count; for caps far below them the polynomial is not used.
+    const double last = std::fabs(power / (k * k) * fit[3]);
+    s.cap_limit = (float)((last < 1e-30 ? 0.02 : last > 1e30 ? 0.0 : 0.5) / k);
     return s;
 }
 
@@ -485,7 +488,9 @@ static pod_status forward_impl(const void *prefill_q, const void *decode_q, cons
     auto go = [&](int which, const pod::KernelArgs &args, hipStream_t on) {
         if (which == pod::kLaunchCombine && no_combine) return;
         if (e != hipSuccess) return;
-        e = p.scored ? pod::launch_scored(which, make_scored(p, args, workspace), dt, hd, on) : pod::launch(which, args, dt, hd, on);
+        if (!p.scored) e = pod::launch(which, args, dt, hd, on);
+        else if (p.logit_cap > 0.f) e = pod::launch_capped(which, make_capped(p, make_scored(p, args, workspace)), dt, hd, on);
+        else e = pod::launch_scored(which, make_scored(p, args, workspace), dt, hd, on);
     };
 
     // The combine pass only touches rows whose partials were produced in this call; the row list
@@ -551,7 +556,7 @@ static pod_status forward_impl(const void *prefill_q, const void *decode_q, cons
             }
             break;
         }
-        if (cta_parallel) {
+        if (cta_parallel || (p.cta_pays && !p.trace && !p.evlog)) {
             // one workgroup per work item: every decode workgroup is given its four units by index
             pod::KernelArgs c = a;
             c.n_static_seats = c.n_dctas;

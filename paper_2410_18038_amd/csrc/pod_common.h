@@ -217,9 +217,12 @@ struct KernelArgs {
 struct ScoredArgs : KernelArgs {
     const int32_t *ranges;                 // [row of out][2]: first visible key and end; first >= end: none
     const float *slopes;                   // [n_q_heads + kMaxGroup] slope * log2(e), or null
-    float cap_log2;                        // logit_cap * log2(e); 0: not capped
     const int32_t *zero_rows;              // decode rows that see no key
     int32_t n_zero_rows;
+};
+// The same with scores capped by a tanh.
+struct CappedArgs : ScoredArgs {
+    float cap_log2;                        // logit_cap * log2(e)
     float cap_exp;                         // 2 * log2(e) * softmax_scale / logit_cap
     float cap_limit;                       // the polynomial holds for dot products up to this,
     float cap_poly[4];                     // and is s * (cap_poly[0] + cap_poly[1] s^2 + ...)

@@ -217,8 +217,9 @@ template <int D> struct PrefillLds {
     static constexpr int kBytes = 4 * kTileBytes;          // K[2] then V[2]
 };
 
-// Whether the arguments are those of changed scores.
-template <class A> constexpr bool kScored = std::is_same<A, ScoredArgs>::value;
+// Whether the arguments are those of changed scores, and of capped ones.
+template <class A> constexpr bool kScored = std::is_base_of<ScoredArgs, A>::value;
+template <class A> constexpr bool kCapped = std::is_same<A, CappedArgs>::value;
 
 // Smallest of a value over the 32 query rows of a wavefront (both halves hold the same rows), in a scalar register.
 __device__ __forceinline__ int wave_min32(int x)
@@ -230,7 +231,7 @@ __device__ __forceinline__ int wave_min32(int x)
 
 // What a score (the dot product, with its bias, or a capped one) is multiplied by to be in units of log2(e).
 __device__ __forceinline__ float score_unit(const KernelArgs &a) { return a.scale_log2; }
-__device__ __forceinline__ float score_unit(const ScoredArgs &a) { return a.cap_log2 != 0.f ? 1.f : a.scale_log2; }
+__device__ __forceinline__ float score_unit(const CappedArgs &) { return 1.f; }
 
 // Caps scores: from dot products to cap * tanh(s / cap) in units of log2(e).  Where all scores of the wavefront are below
 // half of the cap, which is what a cap is for, s times a polynomial in s^2 (within 2^-20.8 of the score: the relative
@@ -238,22 +239,30 @@ __device__ __forceinline__ float score_unit(const ScoredArgs &a) { return a.cap_
 // where e^2y overflows or vanishes as well.  An element is five instructions, or seven with two of a quarter rate: prefill
 // of 2048 tokens at 32K, 32 / 4 heads of 128 channels, POLY / EXP us.
 template <class V, int NB>
-__device__ __forceinline__ void cap_scores(const ScoredArgs &a, V (&s)[NB])
+__device__ __forceinline__ bool polynomial_holds(const CappedArgs &a, const V (&s)[NB])
 {
-    constexpr int E = sizeof(V) / sizeof(float);
     float top = 0.f;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int r = 0; r < E; ++r) top = fmaxf(top, fabsf(s[b][r]));
-    if (__builtin_amdgcn_ballot_w64(top > a.cap_limit) == 0) {
+        for (int r = 0; r < (int)(sizeof(V) / sizeof(float)); ++r) top = fmaxf(top, fabsf(s[b][r]));
+    return __builtin_amdgcn_ballot_w64(top > a.cap_limit) == 0;
+}
+// `less` is taken from the result, in the same instruction.
+__device__ __forceinline__ float cap_polynomial(const CappedArgs &a, float x, float less)
+{
+    const float t = x * x;
+    return __builtin_fmaf(x, __builtin_fmaf(t, __builtin_fmaf(t, __builtin_fmaf(t, a.cap_poly[3], a.cap_poly[2]), a.cap_poly[1]), a.cap_poly[0]), -less);
+}
+template <class V, int NB>
+__device__ __forceinline__ void cap_scores(const CappedArgs &a, V (&s)[NB], bool polynomial)
+{
+    constexpr int E = sizeof(V) / sizeof(float);
+    if (polynomial) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int r = 0; r < E; ++r) {
-                const float x = s[b][r], t = x * x;
-                s[b][r] = x * __builtin_fmaf(t, __builtin_fmaf(t, __builtin_fmaf(t, a.cap_poly[3], a.cap_poly[2]), a.cap_poly[1]), a.cap_poly[0]);
-            }
+            for (int r = 0; r < E; ++r) s[b][r] = cap_polynomial(a, s[b][r], 0.f);
     } else {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -341,7 +350,7 @@ template <int DT, int D, int LAYOUT, class A>
 __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem it,
                                                  unsigned char *smem)
 {
-    constexpr bool SCORED = kScored<A>;
+    constexpr bool SCORED = kScored<A>, CAPPED = kCapped<A>;
     using N = Num<DT>;
     using v8 = typename N::v8;
     using L = PrefillLds<D>;
@@ -395,7 +404,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
             const int32_t *range = a.ranges + 2 * (int64_t)(q_start + tok);
             first = range[0];
             last = range[1] - 1;
-            if (a.slopes) slope = a.slopes[hq] * (a.cap_log2 != 0.f ? 1.f : 1.f / a.scale_log2);
+            if (a.slopes) slope = a.slopes[hq] * (CAPPED ? 1.f : 1.f / a.scale_log2);
         }
         if (row_ok && first > last && it.split == 0) {
             typename N::elem *op = (typename N::elem *)a.out + ((int64_t)(q_start + tok) * a.n_q_heads + hq) * D;
@@ -618,7 +627,9 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
 
     // S^T = K Q^T for one tile: rows = keys, columns = this wavefront's query rows.
     // Register r of block tb holds key j0 + tb*32 + 8*(r/4) + 4*h + r%4.
-    auto scores = [&](int kbuf, f32x16 (&s)[NTB], [[maybe_unused]] int j0) {
+    // (Products that start from a bias are a block of their own: the others start from nothing, for free.)
+    auto products = [&](int kbuf, f32x16 (&s)[NTB], [[maybe_unused]] auto biased, [[maybe_unused]] int j0) __attribute__((always_inline)) {
+        if constexpr (decltype(biased)::value) start_from_bias(s, slope, j0 + 4 * h - key_of_row, j0 + T <= wave_minown);
         const POD_LDS unsigned char *kb = lds + kbuf * L::kTileBytes;
         uint32_t k_base = k_rd0;
         asm("" : "+v"(k_base));                   // opaque copy: the XORs below stay inside the loop
@@ -633,12 +644,12 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
         v8 kk[kOps];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) kk[i] = k_frag(i);
+        if constexpr (!decltype(biased)::value) {
 #pragma unroll
-        for (int tb = 0; tb < NTB; ++tb)
+            for (int tb = 0; tb < NTB; ++tb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[tb][r] = 0.f;
-        if constexpr (SCORED)
-            if (a.slopes && a.cap_log2 == 0.f) start_from_bias(s, slope, j0 + 4 * h - key_of_row, j0 + T <= wave_minown);
+                for (int r = 0; r < 16; ++r) s[tb][r] = 0.f;
+        }
 #pragma unroll
         for (int i = 0; i < kOps; ++i) {
             if (i + kAhead < kOps) kk[i + kAhead] = k_frag(i + kAhead);
@@ -651,6 +662,41 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+    };
+
+    auto scores = [&](int kbuf, f32x16 (&s)[NTB], int j0) __attribute__((always_inline)) {
+        if constexpr (SCORED && !CAPPED) {
+            if (a.slopes) { products(kbuf, s, std::true_type{}, j0); return; }
+        }
+        products(kbuf, s, std::false_type{}, j0);
+    };
+    // The same, with the polynomial cap of the tile before in the shadow of the matrix instructions: its VALU work is as long
+    // are.  (`less`: what the polynomial takes off.)
+    [[maybe_unused]] auto scores_capping = [&](int kbuf, f32x16 (&s)[NTB], [[maybe_unused]] f32x16 (&s_before)[NTB], [[maybe_unused]] float less) {
+        if constexpr (CAPPED) {
+            const POD_LDS unsigned char *kb = lds + kbuf * L::kTileBytes;
+            uint32_t k_base = k_rd0;
+            asm("" : "+v"(k_base));
+            constexpr int kAhead = 3, kOps = NTB * KS, kPerOp = NTB * 16 / kOps;
+            auto k_frag = [&](int i) __attribute__((always_inline)) {
+                return *(const POD_LDS v8 *)(kb + (i / KS) * 32 * L::kRowBytes + (k_base ^ (uint32_t)((i % KS) << 5)));
+            };
+            v8 kk[kOps];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) kk[i] = k_frag(i);
+#pragma unroll
+            for (int tb = 0; tb < NTB; ++tb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[tb][r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kOps; ++i) {
+                if (i + kAhead < kOps) kk[i + kAhead] = k_frag(i + kAhead);
+                s[i / KS] = N::mfma32(kk[i], q[i % KS], s[i / KS]);
+#pragma unroll
+                for (int e = i * kPerOp; e < (i + 1) * kPerOp; ++e) s_before[e / 16][e % 16] = cap_polynomial(a, s_before[e / 16][e % 16], less);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
     };
 
     if (n_tiles <= 0) return;                                // a block of rows that see nothing (or never planned)
@@ -715,27 +761,40 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
         }
         // Matrix blocks ask for issue before the other wavefront's softmax: the two then settle into
         // opposite phases.  (At 256 channels raised priority costs the decode stream more; see the worker.)
+        // Capped scores: already so, and relative to `base`, the running maximum before this tile, where no bias follows.
+        [[maybe_unused]] bool polynomial = false, capped = false, relative = false;
+        [[maybe_unused]] float base = 0.f;
+        if constexpr (CAPPED) {
+            if (live) polynomial = polynomial_holds(a, s_cur);
+            capped = polynomial && next_live;
+            relative = capped && !a.slopes;
+            if (relative && m_run != neg_inf()) base = m_run;
+        }
         if constexpr (D <= 128) __builtin_amdgcn_s_setprio(3);
-        if (next_live) scores(cur ^ 1, s_next, j0 + T);              // matrix unit: scores of the next tile
+        if (CAPPED && capped) scores_capping(cur ^ 1, s_next, s_cur, base);
+        else if (next_live) scores(cur ^ 1, s_next, j0 + T); // matrix unit: scores of the next tile
         if constexpr (D <= 128) __builtin_amdgcn_s_setprio(2);
         if (live) {
             // vector ALUs: softmax of the current tile
             bool need_mask = (j0 + T - 1 > wave_minpos) || (j0 + T > it.kv_end);
             if constexpr (SCORED) {
                 need_mask = need_mask || j0 < wave_maxfirst;
-                if (a.cap_log2 != 0.f) {
-                    cap_scores(a, s_cur);
+                if constexpr (CAPPED) {
+                    if (!capped) cap_scores(a, s_cur, polynomial);
                     if (a.slopes) add_bias(s_cur, slope, j0 + 4 * h - key_of_row);
                 }
             }
             if (__builtin_expect(need_mask, 0)) {
                 const int lim = min(pos, it.kv_end - 1);
+                // (one comparison for both ends of a row's interval: two need a pair of scalar registers an element)
+                [[maybe_unused]] const uint32_t ahead = (uint32_t)(j0 + 4 * h) - (uint32_t)(lim < first ? 0x7fffffff : first);
+                [[maybe_unused]] const uint32_t span = lim < first ? 0u : (uint32_t)lim - (uint32_t)first;
 #pragma unroll
                 for (int tb = 0; tb < NTB; ++tb)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int key = j0 + tb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-                        if (key > lim || (SCORED && key < first)) s_cur[tb][r] = neg_inf();
+                        if (SCORED ? ahead + (uint32_t)(tb * 32 + 8 * (r >> 2) + (r & 3)) > span : key > lim) s_cur[tb][r] = neg_inf();
                     }
             }
             float mx = neg_inf();
@@ -744,6 +803,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
 #pragma unroll
                 for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s_cur[tb][r]);
             mx = max_across_32(mx) * c;
+            if constexpr (CAPPED) mx += base;
             const bool grow = mx > m_run + kMaxSlack;        // also true for the first visible key
             if (__builtin_amdgcn_ballot_w64(grow) != 0) {
                 const float alpha = grow ? fast_exp2(m_run - mx) : 1.f;   // mx is finite where grow holds
@@ -753,8 +813,60 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
                 for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[mb][r] *= alpha;
+                if constexpr (CAPPED) {
+                    const float moved = relative && grow ? m_run - base : 0.f;
+#pragma unroll
+                    for (int tb = 0; tb < NTB; ++tb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s_cur[tb][r] -= moved;
+                }
             }
             const float m_use = (m_run == neg_inf()) ? 0.f : m_run;
+            if constexpr (CAPPED) {
+                // The second product goes key block by key block here, and the weights of a block are worked out in the shadow
+                // of the one before: the vector work of a capped tile is longer than its matrix work.
+                if (!relative) {
+#pragma unroll
+                    for (int tb = 0; tb < NTB; ++tb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s_cur[tb][r] -= m_use;
+                }
+                const POD_LDS unsigned char *vb = lds + (2 + cur) * L::kTileBytes;
+                uint32_t v_base = v_rd0;
+                asm("" : "+v"(v_base));
+                constexpr int kBlocks = 2 * NTB, kOps = kBlocks * MB, kAheadV = 2, kPerOp = 8 / MB;
+                auto v_frag = [&](int j) __attribute__((always_inline)) {
+                    const POD_LDS unsigned char *vp = vb + (j / MB) * 16 * L::kRowBytes + (v_base ^ (uint32_t)((cb0 + j % MB) << 6));
+                    return __builtin_bit_cast(v8, __builtin_shufflevector(lds_read_tr(vp), lds_read_tr(vp + 8 * L::kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7));
+                };
+                v8 vv[kOps], pk[kBlocks];
+#pragma unroll
+                for (int j = 0; j < kAheadV; ++j) vv[j] = v_frag(j);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pk[0][e] = (typename N::elem)fast_exp2(s_cur[0][e]);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (D <= 128) __builtin_amdgcn_s_setprio(3);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    u32x4 pw = __builtin_bit_cast(u32x4, pk[b]);
+                    asm("" : "+v"(pw));                          // packed once, for both uses
+                    l_run = N::add_all(u32x2{pw[0], pw[1]}, l_run);
+                    l_run = N::add_all(u32x2{pw[2], pw[3]}, l_run);
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) {
+                        const int j = b * MB + mb;
+                        if (j + kAheadV < kOps) vv[j + kAheadV] = v_frag(j + kAheadV);
+                        o[mb] = N::mfma32(vv[j], __builtin_bit_cast(v8, pw), o[mb]);
+                        if (b + 1 < kBlocks) {
+#pragma unroll
+                            for (int e = mb * kPerOp; e < (mb + 1) * kPerOp; ++e)
+                                pk[b + 1][e] = (typename N::elem)fast_exp2(s_cur[(b + 1) >> 1][((b + 1) & 1) * 8 + e]);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                if constexpr (D <= 128) __builtin_amdgcn_s_setprio(2);
+            } else {
             v8 pk[NTB][2];
 #pragma unroll
             for (int tb = 0; tb < NTB; ++tb)
@@ -807,6 +919,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
             }
             __builtin_amdgcn_sched_group_barrier(0x008, kAheadV, 0);
             if constexpr (D <= 128) __builtin_amdgcn_s_setprio(2);
+            }
         }
         wait_all_loads();                                    // K tile jt+2 and V tile jt+1 have landed
         __syncthreads();                                     // ... for every wavefront; tile jt is done
@@ -840,9 +953,11 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
             m_run = neg_inf();
             l_run = f32x4{0.f, 0.f, 0.f, 0.f};
             const int lim = min(pos, it.kv_end - 1);
+            const uint32_t span = lim < first ? 0u : (uint32_t)lim - (uint32_t)first;
 #pragma unroll 1
             for (int jt = 0; jt < n_tiles; ++jt) {
                 const int j0 = kv_base + jt * T;
+                const uint32_t ahead = (uint32_t)(j0 + 4 * h) - (uint32_t)(lim < first ? 0x7fffffff : first);
                 __syncthreads();
                 issue_tile(jt, 0, true, true);
                 wait_all_loads();
@@ -850,8 +965,8 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
                 if (j0 > wave_maxpos || j0 + T <= wave_minfirst) continue;
                 f32x16 s[NTB];
                 scores(0, s, j0);
-                if (a.cap_log2 != 0.f) {
-                    cap_scores(a, s);
+                if constexpr (CAPPED) {
+                    cap_scores(a, s, polynomial_holds(a, s));
                     if (a.slopes) add_bias(s, slope, j0 + 4 * h - key_of_row);
                 }
                 float mx = neg_inf();
@@ -859,8 +974,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
                 for (int tb = 0; tb < NTB; ++tb)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const int key = j0 + tb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-                        if (key > lim || key < first) s[tb][r] = neg_inf();
+                        if (ahead + (uint32_t)(tb * 32 + 8 * (r >> 2) + (r & 3)) > span) s[tb][r] = neg_inf();
                         mx = fmaxf(mx, s[tb][r]);
                     }
                 mx = max_across_32(mx) * c;
@@ -881,8 +995,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
 #pragma unroll
                         for (int k = 1; k < 2 * NTB; ++k) x = half == k ? s[k >> 1][(k & 1) * 8 + e] : x;
                         p[e] = __builtin_bit_cast(short, (typename N::elem)fast_exp2(__builtin_fmaf(x, c, -m_use)));
-                        const int key = j0 + 16 * half + 8 * (e >> 2) + 4 * h + (e & 3);
-                        seen[e] = key <= lim && key >= first ? N::kOne : (short)0;
+                        seen[e] = ahead + (uint32_t)(16 * half + 8 * (e >> 2) + (e & 3)) <= span ? N::kOne : (short)0;
                     }
                     const u32x4 pw = __builtin_bit_cast(u32x4, p);
                     l_run = N::add_all(u32x2{pw[0], pw[1]}, l_run);
@@ -1147,7 +1260,7 @@ template <int DT, int D, int LAYOUT, bool MERGE, class A>
 __device__ __forceinline__ int decode_worker_run(const A &a, unsigned char *smem, const int seat,
                                                  const int xcd)
 {
-    constexpr bool SCORED = kScored<A>;
+    constexpr bool SCORED = kScored<A>, CAPPED = kCapped<A>;
     using N = Num<DT>;
     using v8 = typename N::v8;
     using elem = typename N::elem;
@@ -1417,7 +1530,7 @@ __device__ __forceinline__ int decode_worker_run(const A &a, unsigned char *smem
                 float x = 0.f;
 #pragma unroll
                 for (int g = 0; g < kMaxGroup; ++g) x = n16 == g ? sl[g] : x;    // (kMaxGroup more are there than heads)
-                slope = x * (a.cap_log2 != 0.f ? 1.f : 1.f / a.scale_log2);
+                slope = x * (CAPPED ? 1.f : 1.f / a.scale_log2);
                 key_of_row = ((const POD_CONST int32_t *)a.seq_meta)[4 * d.req + 2] - 1;
             }
         }
@@ -1448,21 +1561,22 @@ __device__ __forceinline__ int decode_worker_run(const A &a, unsigned char *smem
         }
         const int n_valid = min(cu.t1 - t_first, STEP) - 4 * b4;         // keys of this lane that exist
         if constexpr (SCORED) {
-            const int n_ahead = cu.t0 - t_first - 4 * b4;                // ... of which these are ahead of the unit's first key
-            if (a.cap_log2 != 0.f) {
+            const uint32_t ahead = (uint32_t)(t_first + 4 * b4) - (uint32_t)cu.t0, span = (uint32_t)(cu.t1 - 1 - cu.t0);   // (see the prefill loop)
+            if constexpr (CAPPED) {
                 f32x4 one[1] = {s};
-                cap_scores(a, one);
+                cap_scores(a, one, polynomial_holds(a, one));
                 s = one[0];
             }
             const float base = (float)(t_first + 4 * b4 - key_of_row);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (a.slopes) s[r] = __builtin_fmaf(-slope, fabsf(base + (float)r), s[r]);
-                s[r] = (r >= n_ahead) ? s[r] : neg_inf();
+                s[r] = ahead + (uint32_t)r <= span && (STEP == 16 || 4 * b4 < STEP) ? s[r] : neg_inf();
             }
-        }
+        } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[r] = (r < n_valid) ? s[r] : neg_inf();
+            for (int r = 0; r < 4; ++r) s[r] = (r < n_valid) ? s[r] : neg_inf();
+        }
         float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
         mx = max_across_32(max_across_16(mx)) * c;
         const bool grow = mx > m_run + kMaxSlack;          // also true for the first key
@@ -2067,7 +2181,26 @@ __device__ __forceinline__ void fused_workgroup(const A a)
         const int seat = bind[1];
         return seat;
     };
-    if (first == kPrefill) {
+    if constexpr (kScored<std::remove_cv_t<std::remove_reference_t<A>>>) {
+        // (Each operation once in the code: twice it takes more scalar registers than there are, and their reloads sit in the loops.)
+        n_first = n_second = 0;
+#pragma unroll 1
+        for (int turn = 0; turn < 2; ++turn) {
+            int n;
+            if ((first == kPrefill) == (turn == 0)) {
+                n = prefill_worker_run<DT, D, LAYOUT>(a, smem, &bind[4], xcd);
+            } else {
+                const int seat = take_seat();
+                n = seat < a.n_dwgs ? decode_worker_run<DT, D, LAYOUT, MERGE>(a, smem, seat, xcd) : 0;
+            }
+            if (turn == 0) {
+                n_first = n;
+                if (a.trace) t_switch = wall_clock64();
+            } else {
+                n_second = n;
+            }
+        }
+    } else if (first == kPrefill) {
         n_first = prefill_worker_run<DT, D, LAYOUT>(a, smem, &bind[4], xcd);
         if (a.trace) t_switch = wall_clock64();
         const int seat = take_seat();
@@ -2252,14 +2385,14 @@ __global__ __launch_bounds__(kWgThreads) void combine_kernel(KernelArgs a)
 // The kernels of plans with changed scores: the same workgroups with the scores capped, falling with distance or masked by
 // an interval of keys per row.
 // ------------------------------------------------------------------------------------------
-template <int DT, int D, int LAYOUT>
-__global__ __launch_bounds__(kWgThreads, 2) void prefill_scored(ScoredArgs a) { prefill_workgroup<DT, D, LAYOUT, const ScoredArgs &>(a); }
-template <int DT, int D, int LAYOUT>
-__global__ __launch_bounds__(kWgThreads, 2) void decode_scored(ScoredArgs a) { decode_workgroup<DT, D, LAYOUT, false, const ScoredArgs &>(a); }
-template <int DT, int D, int LAYOUT>
-__global__ __launch_bounds__(kWgThreads, 2) void fused_scored(ScoredArgs a) { fused_workgroup<DT, D, LAYOUT, false, const ScoredArgs &>(a); }
-template <int DT, int D, int LAYOUT>
-__global__ __launch_bounds__(kWgThreads, 2) void fused_cta_scored(ScoredArgs a) { fused_cta_workgroup<DT, D, LAYOUT, false, const ScoredArgs &>(a); }
+template <int DT, int D, int LAYOUT, class A>
+__global__ __launch_bounds__(kWgThreads, 2) void prefill_scored(A a) { prefill_workgroup<DT, D, LAYOUT, const A &>(a); }
+template <int DT, int D, int LAYOUT, class A>
+__global__ __launch_bounds__(kWgThreads, 2) void decode_scored(A a) { decode_workgroup<DT, D, LAYOUT, false, const A &>(a); }
+template <int DT, int D, int LAYOUT, class A>
+__global__ __launch_bounds__(kWgThreads, 2) void fused_scored(A a) { fused_workgroup<DT, D, LAYOUT, false, const A &>(a); }
+template <int DT, int D, int LAYOUT, class A>
+__global__ __launch_bounds__(kWgThreads, 2) void fused_cta_scored(A a) { fused_cta_workgroup<DT, D, LAYOUT, false, const A &>(a); }
 // Decode rows that see no key have no unit; their results are zeros.  (16 bytes a thread, a row a workgroup.)
 template <int D>
 __global__ __launch_bounds__(kWgThreads) void zero_decode_rows(void *out, const int32_t *rows, int64_t first_row, int n_q_heads)
@@ -2343,22 +2476,22 @@ static hipError_t launch_variant(int which, const KernelArgs &a, hipStream_t str
     return hipGetLastError();
 }
 
-template <int DT, int D, int LAYOUT>
-static hipError_t launch_scored_variant(int which, const ScoredArgs &a, hipStream_t stream)
+template <int DT, int D, int LAYOUT, class A>
+static hipError_t launch_scored_variant(int which, const A &a, hipStream_t stream)
 {
     const dim3 threads(kWgThreads);
     switch (which) {
     case kLaunchPrefill:
-        if (a.n_pitems > 0) prefill_scored<DT, D, LAYOUT><<<dim3(a.n_pitems), threads, 0, stream>>>(a);
+        if (a.n_pitems > 0) prefill_scored<DT, D, LAYOUT, A><<<dim3(a.n_pitems), threads, 0, stream>>>(a);
         break;
     case kLaunchDecode:
-        if (a.n_dwgs > 0) decode_scored<DT, D, LAYOUT><<<dim3(a.n_dwgs), threads, 0, stream>>>(a);
+        if (a.n_dwgs > 0) decode_scored<DT, D, LAYOUT, A><<<dim3(a.n_dwgs), threads, 0, stream>>>(a);
         break;
     case kLaunchFused:
-        if (a.fused_grid > 0) fused_scored<DT, D, LAYOUT><<<dim3(a.fused_grid), threads, 0, stream>>>(a);
+        if (a.fused_grid > 0) fused_scored<DT, D, LAYOUT, A><<<dim3(a.fused_grid), threads, 0, stream>>>(a);
         break;
     case kLaunchFusedCta:
-        if (a.n_pitems + a.n_dctas > 0) fused_cta_scored<DT, D, LAYOUT><<<dim3(a.n_pitems + a.n_dctas), threads, 0, stream>>>(a);
+        if (a.n_pitems + a.n_dctas > 0) fused_cta_scored<DT, D, LAYOUT, A><<<dim3(a.n_pitems + a.n_dctas), threads, 0, stream>>>(a);
         break;
     case kLaunchZeroRows:
         if (a.n_zero_rows > 0)
@@ -2370,8 +2503,8 @@ static hipError_t launch_scored_variant(int which, const ScoredArgs &a, hipStrea
     return hipGetLastError();
 }
 
-template <int DT, int D>
-hipError_t launch_scored_layout(int which, const ScoredArgs &a, int layout, hipStream_t stream)
+template <int DT, int D, class A>
+hipError_t launch_scored_layout(int which, const A &a, int layout, hipStream_t stream)
 {
     switch (layout) {
     case kLayoutContiguous: return launch_scored_variant<DT, D, kLayoutContiguous>(which, a, stream);
@@ -2394,10 +2527,10 @@ hipError_t launch_layout(int which, const KernelArgs &a, int layout, hipStream_t
     }
 }
 
-// This file is compiled twice per (16-bit type, head_dim), which hold the kernels of that pair and those of changed
-// scores, and once without, which holds the rest: the compilations run side by side.
+// This file is compiled three times per (16-bit type, head_dim), which hold the kernels of that pair, those of changed
+// scores and those of capped ones, and once without, which holds the rest: the compilations run side by side.
 #if defined(POD_INSTANCE_SCORED)
-template hipError_t launch_scored_layout<POD_INSTANCE_DT, POD_INSTANCE_D>(int, const ScoredArgs &, int, hipStream_t);
+template hipError_t launch_scored_layout<POD_INSTANCE_DT, POD_INSTANCE_D>(int, const POD_INSTANCE_SCORED &, int, hipStream_t);
 #elif defined(POD_INSTANCE_DT)
 template hipError_t launch_layout<POD_INSTANCE_DT, POD_INSTANCE_D>(int, const KernelArgs &, int, hipStream_t);
 #else
@@ -2408,14 +2541,15 @@ extern template hipError_t launch_layout<1, 64>(int, const KernelArgs &, int, hi
 extern template hipError_t launch_layout<1, 128>(int, const KernelArgs &, int, hipStream_t);
 extern template hipError_t launch_layout<1, 256>(int, const KernelArgs &, int, hipStream_t);
 
-extern template hipError_t launch_scored_layout<0, 64>(int, const ScoredArgs &, int, hipStream_t);
-extern template hipError_t launch_scored_layout<0, 128>(int, const ScoredArgs &, int, hipStream_t);
-extern template hipError_t launch_scored_layout<0, 256>(int, const ScoredArgs &, int, hipStream_t);
-extern template hipError_t launch_scored_layout<1, 64>(int, const ScoredArgs &, int, hipStream_t);
-extern template hipError_t launch_scored_layout<1, 128>(int, const ScoredArgs &, int, hipStream_t);
-extern template hipError_t launch_scored_layout<1, 256>(int, const ScoredArgs &, int, hipStream_t);
 
-hipError_t launch_scored(int which, const ScoredArgs &a, int dtype, int head_dim, hipStream_t stream)
+#define POD_SCORED(DT, D)                                                                                        \
+    extern template hipError_t launch_scored_layout<DT, D>(int, const ScoredArgs &, int, hipStream_t);           \
+    extern template hipError_t launch_scored_layout<DT, D>(int, const CappedArgs &, int, hipStream_t)
+POD_SCORED(0, 64); POD_SCORED(0, 128); POD_SCORED(0, 256); POD_SCORED(1, 64); POD_SCORED(1, 128); POD_SCORED(1, 256);
+#undef POD_SCORED
+
+template <class A>
+static hipError_t launch_changed(int which, const A &a, int dtype, int head_dim, hipStream_t stream)
 {
     if (which == kLaunchCombine) return launch(which, a, dtype, head_dim, stream);
     const int layout = cache_layout(a.block_size, head_dim, a.n_kv_heads);
@@ -2427,6 +2561,8 @@ hipError_t launch_scored(int which, const ScoredArgs &a, int dtype, int head_dim
     if (dtype == 1 && head_dim == 256) return launch_scored_layout<1, 256>(which, a, layout, stream);
     return hipErrorInvalidValue;
 }
+hipError_t launch_scored(int which, const ScoredArgs &a, int dtype, int head_dim, hipStream_t stream) { return launch_changed(which, a, dtype, head_dim, stream); }
+hipError_t launch_capped(int which, const CappedArgs &a, int dtype, int head_dim, hipStream_t stream) { return launch_changed(which, a, dtype, head_dim, stream); }
 
 __global__ void clear_header_kernel(WsHeader *hdr)
 {

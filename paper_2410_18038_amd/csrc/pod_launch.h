@@ -14,6 +14,7 @@ enum LaunchKind : int { kLaunchPrefill = 0, kLaunchDecode = 1, kLaunchFused = 2,
 hipError_t launch(int which, const KernelArgs &a, int dtype, int head_dim, hipStream_t stream);
 // The same for a plan with changed scores (not the kinds of the prefill-heavy configuration).
 hipError_t launch_scored(int which, const ScoredArgs &a, int dtype, int head_dim, hipStream_t stream);
+hipError_t launch_capped(int which, const CappedArgs &a, int dtype, int head_dim, hipStream_t stream);
 // Zero the counters at the head of a workspace.
 hipError_t clear_header(WsHeader *hdr, hipStream_t stream);
 

@@ -732,7 +732,12 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         for (int r = 0; r < n_req; ++r) {
             const double q_len = seq_meta[4 * r + 1], kv_len = seq_meta[4 * r + 2];
             kv_tokens += kv_len;
-            if (r < prm.n_prefill) pairs += q_len * (kv_len - q_len) + q_len * (q_len + 1.0) / 2.0;
+            if (plan.scored && r < prm.n_prefill) {
+                for (int i = 0; i < seq_meta[4 * r + 1]; ++i) {
+                    const int32_t *range = plan.ranges.data() + 2 * ((size_t)seq_meta[4 * r] + (size_t)i);
+                    pairs += std::max(0, range[1] - range[0]);
+                }
+            } else if (r < prm.n_prefill) pairs += q_len * (kv_len - q_len) + q_len * (q_len + 1.0) / 2.0;
         }
         const double flop_time = 4.0 * prm.head_dim * pairs * prm.n_q_heads / 2.5e15;
         const double byte_time = kv_tokens * prm.n_kv_heads * prm.head_dim * 4.0 / 8.0e12;
@@ -750,13 +755,18 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         // 279; an item for every second slot (210, 1.04) 737 / 735.  (Towards long decode streams the two are level somewhere
         // between 0.24 and 0.54; the line keeps clear of that.)
         double decode_tokens = 0.0;
-        for (int r = prm.n_prefill; r < n_req; ++r) decode_tokens += seq_meta[4 * r + 2];
+        for (int r = prm.n_prefill; r < n_req; ++r) decode_tokens += keys[(size_t)r];
         const double decode_time = decode_tokens * prm.n_kv_heads * prm.head_dim * 4.0 / 8.0e12;
         // (Rates and times are those of the whole chip.  A plan for fewer units keeps to the workgroups of its fused launch,
         // where the prefill kernel has one per item.)
-        plan.heavy_pays = prm.policy == POD_POLICY_AUTO && built && prm.n_decode > 0 && n_cus == kChipUnits &&
-                          (int)plan.pitems.size() >= kSlotsPerUnit * n_cus && flop_time >= 200e-6 &&
-                          flop_time >= 0.8 * decode_time && flop_time <= 3.3 * decode_time;
+        const bool outweighs = prm.policy == POD_POLICY_AUTO && prm.n_decode > 0 && n_cus == kChipUnits &&
+                               (int)plan.pitems.size() >= kSlotsPerUnit * n_cus && flop_time >= 200e-6 &&
+                               flop_time >= 0.8 * decode_time && flop_time <= 3.3 * decode_time;
+        plan.heavy_pays = built && outweighs;
+        // Changed scores have no such pair of kernels.  Their persistent launch is behind the one of a workgroup per item
+        // there: 2048 tokens at 32K beside 32 x 32K, 32 / 4 heads, 1353 / 1256 us, capped 1537 / 1467 (with an item for every
+        // second slot, 512 tokens beside 64 x 8K, it is ahead, 380 / 436, under a window of 4096 as well, 203 / 210).
+        plan.cta_pays = plan.scored && outweighs && !plan.dunits.empty();
         // Which of the two a fused call runs depends on what other streams do, and its bits must not: the light decode kernel
         // leaves merging to the combine kernel, which adds the weights in another order, so the units of the default
         // configuration do as well.  (Only decode units of a given length come here: cut by the planner, streams as long as

@@ -34,6 +34,7 @@ struct Plan {
     // Plans with changed scores: the interval of visible keys of each row of `out` (first, end), slopes * log2(e) with
     // kMaxGroup zeros behind them (empty: none), and the decode rows that see nothing.
     bool scored = false;
+    bool cta_pays = false;                  // POD_MODE_FUSED launches one workgroup per work item
     float logit_cap = 0.f;
     std::vector<int32_t> ranges;
     std::vector<float> slopes;
