@@ -236,8 +236,8 @@ __device__ __forceinline__ float score_unit(const CappedArgs &) { return 1.f; }
 // Caps scores: from dot products to cap * tanh(s / cap) in units of log2(e).  Where all scores of the wavefront are below
 // half of the cap, which is what a cap is for, s times a polynomial in s^2 (within 2^-20.8 of the score: the relative
 // minimax fit of tanh y / y with four terms on |y| <= 1/2); otherwise 1 - 2 / (1 + e^2y), which is within 2^-22 of the cap,
-// where e^2y overflows or vanishes as well.  An element is five instructions, or seven with two of a quarter rate: prefill
-// of 2048 tokens at 32K, 32 / 4 heads of 128 channels, POLY / EXP us.
+// where e^2y overflows or vanishes as well.  An element is five instructions, or five and two of a quarter rate: prefill of
+// 2048 tokens at 32K, 32 / 4 heads of 128 channels, 1202 / 1375 us.
 template <class V, int NB>
 __device__ __forceinline__ bool polynomial_holds(const CappedArgs &a, const V (&s)[NB])
 {
@@ -670,8 +670,12 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
         }
         products(kbuf, s, std::false_type{}, j0);
     };
-    // The same, with the polynomial cap of the tile before in the shadow of the matrix instructions: its VALU work is as long
-    // are.  (`less`: what the polynomial takes off.)
+    // The same, with the polynomial cap of the tile before in the shadow of the matrix instructions.  (`less`: what the
+    // polynomial takes off.)  A wavefront by itself gets every second slot of the vector pipe, so that the two wavefronts of a
+    // SIMD in opposite phases leave half of it empty; the work beside the matrix instructions of the same wavefront does not.
+    // us, cap before the masks / here and the weights beside the second product: 2048 tokens at 32K, 32 / 4 heads, 1229 / 1165
+    // (none 1000), 4096 tokens of 64 channels 155 / 119.  (A biased form of this block, for slopes behind a cap, took 7 % off
+    // those and put 5-10 % on all others: it does not fit the registers beside this one.)
     [[maybe_unused]] auto scores_capping = [&](int kbuf, f32x16 (&s)[NTB], [[maybe_unused]] f32x16 (&s_before)[NTB], [[maybe_unused]] float less) {
         if constexpr (CAPPED) {
             const POD_LDS unsigned char *kb = lds + kbuf * L::kTileBytes;
