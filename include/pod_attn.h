@@ -198,12 +198,15 @@ void       pod_attn_plan_destroy(pod_attn_plan *plan);
  * i.e. a sliding window, documents that do not see each other packed into one request, and a prefix whose tokens everyone
  * in the request sees, from in front as well.  A row with first >= end sees nothing and its result is 0.
  * What a row does not see does not reach its result, be it infinite or NaN, and cache blocks (or parts of them) whose keys
- * no row of the batch sees are not read: their entries in block_table may name no block.
+ * no row of the batch sees are not read: their entries in block_table may name no block.  (Visible values that are infinite
+ * make a result infinite or NaN, as their weighted sum does, or NaN where a decode row re-reads them for keys that do not exist.)
+ * With POD_MODE_FLAG_NO_COMBINE decode rows that see nothing are not written either.
  */
 typedef struct {
-    float   logit_cap;          /* >= 0 and finite; 0: scores are not capped                     */
+    float   logit_cap;          /* >= 0; 0: scores are not capped.  At most 1e20, and within a factor of 1e20 of
+                                   softmax_scale                                                  */
     int32_t window;             /* >= 0; 0: no window                                             */
-    const float   *slopes;      /* host [n_q_heads], finite, or NULL                              */
+    const float   *slopes;      /* host [n_q_heads], finite, or NULL; |slope| <= 1e20 min(1, softmax_scale) */
     const int32_t *doc_start;   /* host [rows of out], >= 0, or NULL                              */
     const int32_t *prefix_len;  /* host [n_prefill + n_decode], >= 0, or NULL                     */
 } pod_attn_scores;
@@ -411,7 +414,7 @@ typedef struct {
  *   rope         host, or NULL: no rotation;  rope_table device, the table above for `rope`
  *   norm         host, or NULL: no normalisation
  *   slots,       device, int32 [n_rows], as pod_attn_build_tables leaves them.  A row with a negative slot, or one beyond
- *   positions    the cache, is padding: nothing of it is read or written.  Rows must not share a slot.
+ *   positions    the cache, is padding: nothing of it is used or written.  Rows must not share a slot.
  *   q_out        device, [n_rows][Hq][d]: prefill_q, and behind the prefill rows decode_q, of the attention call.  May be
  *                q itself where q_stride is Hq * d; must not overlap the inputs otherwise
  *   k_cache, v_cache  the cache of `params`

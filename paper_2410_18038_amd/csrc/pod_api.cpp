@@ -151,7 +151,7 @@ pod::CappedArgs make_capped(const pod::Plan &p, const pod::ScoredArgs &a)
     // Coefficients that leave the range of 32 bits: for caps far above the scores only |y| <= 1/50, where the upper two do
     // not count; for caps far below them the polynomial is not used.
     const double last = std::fabs(power / (k * k) * fit[3]);
-    s.cap_limit = (float)((last < 1e-30 ? 0.02 : last > 1e30 ? 0.0 : 0.5) / k);
+    s.cap_limit = (float)((last < 1e-30 ? 0.02 : last > 1e30 ? -1.0 : 0.5) / k);
     return s;
 }
 

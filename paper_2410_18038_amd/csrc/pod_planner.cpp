@@ -115,6 +115,9 @@ int64_t units_of_length(const pod_attn_params &prm, const std::vector<int32_t> &
 pod_status read_scores(const pod_attn_scores &scores, const pod_attn_params &prm, const int32_t *seq_meta, Plan &plan, std::string &err)
 {
     if (!(scores.logit_cap >= 0.f) || !std::isfinite(scores.logit_cap)) { err = "logit_cap must be finite and not negative"; return POD_ERR_INVALID_ARG; }
+    // (what the kernels work with, scale / cap and slope / scale, has to keep clear of the ends of 32 bits)
+    const double per_cap = scores.logit_cap > 0.f ? (double)prm.softmax_scale / scores.logit_cap : 1.0;
+    if (per_cap < 1e-20 || per_cap > 1e20 || scores.logit_cap > 1e20f) { err = "logit_cap is too far from softmax_scale"; return POD_ERR_INVALID_ARG; }
     if (scores.window < 0) { err = "negative window"; return POD_ERR_INVALID_ARG; }
     const int n_req = prm.n_prefill + prm.n_decode;
     plan.scored = true;
@@ -123,6 +126,10 @@ pod_status read_scores(const pod_attn_scores &scores, const pod_attn_params &prm
         plan.slopes.assign((size_t)prm.n_q_heads + kMaxGroup, 0.f);
         for (int h = 0; h < prm.n_q_heads; ++h) {
             if (!std::isfinite(scores.slopes[h])) { err = fmt("slope of head %lld is not finite", h); return POD_ERR_INVALID_ARG; }
+            if (std::fabs((double)scores.slopes[h]) > 1e20 * std::min(1.0, (double)prm.softmax_scale)) {
+                err = fmt("slope of head %lld is too large", h);
+                return POD_ERR_INVALID_ARG;
+            }
             plan.slopes[(size_t)h] = scores.slopes[h] * 1.4426950408889634f;
         }
     }

@@ -2,8 +2,9 @@
 
 The reference is numpy in 64 bits, straight from the definition in the header.  How far a result may be off follows from
 what is rounded: weights to the 16-bit type before the second product (half a step each, in the sum and in what it is
-divided by), the result (half a step), and scores in 32 bits (2^-19 of a dot product's magnitude, 2^-21 of the cap and of the
-largest bias, as a relative error of the weights); in fp16, weights below 2^-24 of the largest are lost (half of that each).
+divided by), the result (half a step), and scores in 32 bits (2^-19 of a dot product's magnitude, 2^-21 of the cap, or
+2^-20 of the largest score where all are below half of it, and 2^-21 of the largest bias, as a relative error of the
+weights); in fp16, weights below 2^-24 of the largest are lost (half of that each).
 """
 import ctypes
 import dataclasses
@@ -61,6 +62,8 @@ def reference(batch, scores):
         key = np.arange(kv_len)
         seen = (key >= first[rows, None]) & (key < end[rows, None])
         k_all, v_all = logical(batch, batch.k_cache, r), logical(batch, batch.v_cache, r)
+        with np.errstate(invalid="ignore"):
+            raw = [np.nanmax(np.abs(q_all[rows, h] @ k_all[:, h * hkv // hq].T), initial=0) * batch.softmax_scale for h in range(hq)]
         for h in range(hq):
             k, v, q = k_all[:, h * hkv // hq], v_all[:, h * hkv // hq], q_all[rows, h]
             with np.errstate(invalid="ignore"):
@@ -69,7 +72,8 @@ def reference(batch, scores):
             delta = 2.0 ** -19 * np.where(seen, size, 0).max(-1)
             if scores.logit_cap:
                 s = scores.logit_cap * np.tanh(s / scores.logit_cap)
-                delta += 2.0 ** -21 * scores.logit_cap
+                below = np.nanmax(raw) <= 0.45 * scores.logit_cap        # every score of the request: the polynomial's error is relative
+                delta += 2.0 ** -20 * np.where(seen, np.abs(s), 0).max(-1) if below else 2.0 ** -21 * scores.logit_cap
             if scores.slopes is not None:
                 far = np.abs(key - at[rows, None])
                 s = s - scores.slopes[h] * far
@@ -189,6 +193,10 @@ def test_score_arguments_are_checked():
         with pytest.raises(pod.PodError) as e:
             plan(scores)
         assert e.value.status == -1 and len(str(e.value)) > 15
+    for scores in [pod.Scores(logit_cap=1e21), pod.Scores(logit_cap=1e-30), pod.Scores(slopes=[1e25] * 4), pod.Scores(slopes=[0.0, -1e20, 0.0, 0.0])]:
+        with pytest.raises(pod.PodError) as e:
+            plan(scores)
+        assert e.value.status == -1 and "too" in str(e.value)
     for scores in [pod.Scores(slopes=[1.0]), pod.Scores(doc_start=[0]), pod.Scores(prefix_len=[0] * (n_req + 1))]:
         with pytest.raises(ValueError):
             plan(scores)
@@ -333,11 +341,14 @@ def test_split_work_merges_to_the_same_result_in_every_mode(mode, d, block):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [wl.F16, wl.BF16])
-@pytest.mark.parametrize("cap,spread", [(0.5, 1.0), (5.0, 30.0), (50.0, 4.0), (1000.0, 20.0), (30.0, 0.02), (1e6, 1.0)])
+@pytest.mark.parametrize("cap,spread", [(0.5, 1.0), (5.0, 30.0), (50.0, 4.0), (1000.0, 20.0), (30.0, 0.02), (1e6, 1.0),
+                                        (1e-6, 1.0), (1e-18, 1.0), (1e18, 1.0)])
 def test_caps_from_far_below_the_scores_to_far_above(dtype, cap, spread):
     batch = grid_batch(8, 2, 128, dtype, 16, False, decode=(5, 300, 1000))
     batch = dataclasses.replace(batch, prefill_q=(batch.prefill_q.float() * spread).to(batch.torch_dtype),
                                 decode_q=(batch.decode_q.float() * spread).to(batch.torch_dtype))
+    batch.prefill_q[3] = 0                                               # scores of exactly 0
+    batch.decode_q[0] = 0
     check(batch, pod.Scores(logit_cap=cap))
 
 
