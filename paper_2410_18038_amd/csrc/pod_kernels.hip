@@ -224,9 +224,12 @@ template <class A> constexpr bool kCapped = std::is_same<A, CappedArgs>::value;
 // Smallest of a value over the 32 query rows of a wavefront (both halves hold the same rows), in a scalar register.
 __device__ __forceinline__ int wave_min32(int x)
 {
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) x = min(x, __shfl_xor(x, d));
-    return __builtin_amdgcn_readfirstlane(x);
+    x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xf, false));       // within 16 lanes, going round by 8, 4, 2, 1
+    x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x124, 0xf, 0xf, false));
+    x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x122, 0xf, 0xf, false));
+    x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x121, 0xf, 0xf, false));
+    const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+    return __builtin_amdgcn_readfirstlane(min((int)r[0], (int)r[1]));
 }
 
 // What a score (the dot product, with its bias, or a capped one) is multiplied by to be in units of log2(e).
@@ -398,30 +401,36 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
     int first = 0, wave_minfirst = 0, wave_maxfirst = 0, wave_minown = 0;
     float slope = 0.f;
     const int key_of_row = prefix + min(tok, q_len - 1);   // where the row's own token sits
+    int range[2] = {0, 0};
     if constexpr (SCORED) {
-        int last = -1;
         if (row_ok) {
-            const int32_t *range = a.ranges + 2 * (int64_t)(q_start + tok);
-            first = range[0];
-            last = range[1] - 1;
-            if (a.slopes) slope = a.slopes[hq] * (CAPPED ? 1.f : 1.f / a.scale_log2);
+            // (asked for with the queries and the first tiles, looked at when those have arrived)
+            const u32x2 w = *(const u32x2 *)(a.ranges + 2 * (int64_t)(q_start + tok));
+            range[0] = (int)w[0];
+            range[1] = (int)w[1];
+            if (a.slopes) slope = a.slopes[hq];
         }
-        if (row_ok && first > last && it.split == 0) {
-            typename N::elem *op = (typename N::elem *)a.out + ((int64_t)(q_start + tok) * a.n_q_heads + hq) * D;
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                for (int rq = 0; rq < 4; ++rq) *(u32x2 *)(op + (cb0 + mb) * 32 + 8 * rq + 4 * h) = u32x2{0u, 0u};
-        }
-        row_ok = first <= last;
-        pos = row_ok ? last : 0x7fffffff;
-        if (!row_ok) first = 0;
-        wave_minown = wave_min32(key_of_row);
-        wave_minpos = wave_min32(row_ok ? last : 0x7fffffff);
-        wave_maxpos = -wave_min32(row_ok ? -last : 1);
-        wave_minfirst = wave_min32(row_ok ? first : 0x7fffffff);
-        wave_maxfirst = -wave_min32(row_ok ? -first : 0);
     }
+    auto read_range = [&]() __attribute__((always_inline)) {
+        if constexpr (SCORED) {
+            if (row_ok && range[0] >= range[1] && it.split == 0) {
+                typename N::elem *op = (typename N::elem *)a.out + ((int64_t)(q_start + tok) * a.n_q_heads + hq) * D;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int rq = 0; rq < 4; ++rq) *(u32x2 *)(op + (cb0 + mb) * 32 + 8 * rq + 4 * h) = u32x2{0u, 0u};
+            }
+            row_ok = range[0] < range[1];
+            first = row_ok ? range[0] : 0;
+            pos = row_ok ? range[1] - 1 : 0x7fffffff;
+            slope *= CAPPED ? 1.f : 1.f / a.scale_log2;
+            wave_minown = wave_min32(key_of_row);
+            wave_minpos = wave_min32(pos);
+            wave_maxpos = -wave_min32(row_ok ? -pos : 1);
+            wave_minfirst = wave_min32(row_ok ? first : 0x7fffffff);
+            wave_maxfirst = -wave_min32(-first);
+        }
+    };
 
     v8 q[KS];
     {
@@ -703,6 +712,8 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
         }
     };
 
+    if constexpr (SCORED)
+        if (n_tiles <= 0) read_range();
     if (n_tiles <= 0) return;                                // a block of rows that see nothing (or never planned)
     __syncthreads();                                         // previous use of this LDS is over
     TileBases carry = {};                                     // bases of tile jt+1 inside the loop
@@ -728,6 +739,7 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
     // issued just before them have landed.
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[ks]));
+    read_range();
     __syncthreads();
     // Two score buffers swap roles from one tile to the next; the loop body exists twice (even
     // and odd tiles) so that the swap is a matter of names, not of 32 register moves per tile, and
