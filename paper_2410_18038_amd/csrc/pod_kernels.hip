@@ -2403,12 +2403,12 @@ __global__ __launch_bounds__(kWgThreads) void combine_kernel(KernelArgs a)
 // ------------------------------------------------------------------------------------------
 template <int DT, int D, int LAYOUT, class A>
 __global__ __launch_bounds__(kWgThreads, 2) void prefill_scored(A a) { prefill_workgroup<DT, D, LAYOUT, const A &>(a); }
-template <int DT, int D, int LAYOUT, class A>
-__global__ __launch_bounds__(kWgThreads, 2) void decode_scored(A a) { decode_workgroup<DT, D, LAYOUT, false, const A &>(a); }
+template <int DT, int D, int LAYOUT, bool MERGE, class A>
+__global__ __launch_bounds__(kWgThreads, 2) void decode_scored(A a) { decode_workgroup<DT, D, LAYOUT, MERGE, const A &>(a); }
 template <int DT, int D, int LAYOUT, class A>
 __global__ __launch_bounds__(kWgThreads, 2) void fused_scored(A a) { fused_workgroup<DT, D, LAYOUT, false, const A &>(a); }
-template <int DT, int D, int LAYOUT, class A>
-__global__ __launch_bounds__(kWgThreads, 2) void fused_cta_scored(A a) { fused_cta_workgroup<DT, D, LAYOUT, false, const A &>(a); }
+template <int DT, int D, int LAYOUT, bool MERGE, class A>
+__global__ __launch_bounds__(kWgThreads, 2) void fused_cta_scored(A a) { fused_cta_workgroup<DT, D, LAYOUT, MERGE, const A &>(a); }
 // Decode rows that see no key have no unit; their results are zeros.  (16 bytes a thread, a row a workgroup.)
 template <int D>
 __global__ __launch_bounds__(kWgThreads) void zero_decode_rows(void *out, const int32_t *rows, int64_t first_row, int n_q_heads)
@@ -2496,18 +2496,32 @@ template <int DT, int D, int LAYOUT, class A>
 static hipError_t launch_scored_variant(int which, const A &a, hipStream_t stream)
 {
     const dim3 threads(kWgThreads);
+    if (a.arrived && (which == kLaunchDecode || which == kLaunchFused || which == kLaunchFusedCta)) {
+        // the units merge their groups (no plan that does binds by ticket)
+        if constexpr (D <= kMergeDim) {
+            if (which == kLaunchDecode) {
+                if (a.n_dwgs > 0) decode_scored<DT, D, LAYOUT, true, A><<<dim3(a.n_dwgs), threads, 0, stream>>>(a);
+                return hipGetLastError();
+            }
+            if (which == kLaunchFusedCta) {
+                if (a.n_pitems + a.n_dctas > 0) fused_cta_scored<DT, D, LAYOUT, true, A><<<dim3(a.n_pitems + a.n_dctas), threads, 0, stream>>>(a);
+                return hipGetLastError();
+            }
+        }
+        return hipErrorInvalidValue;
+    }
     switch (which) {
     case kLaunchPrefill:
         if (a.n_pitems > 0) prefill_scored<DT, D, LAYOUT, A><<<dim3(a.n_pitems), threads, 0, stream>>>(a);
         break;
     case kLaunchDecode:
-        if (a.n_dwgs > 0) decode_scored<DT, D, LAYOUT, A><<<dim3(a.n_dwgs), threads, 0, stream>>>(a);
+        if (a.n_dwgs > 0) decode_scored<DT, D, LAYOUT, false, A><<<dim3(a.n_dwgs), threads, 0, stream>>>(a);
         break;
     case kLaunchFused:
         if (a.fused_grid > 0) fused_scored<DT, D, LAYOUT, A><<<dim3(a.fused_grid), threads, 0, stream>>>(a);
         break;
     case kLaunchFusedCta:
-        if (a.n_pitems + a.n_dctas > 0) fused_cta_scored<DT, D, LAYOUT, A><<<dim3(a.n_pitems + a.n_dctas), threads, 0, stream>>>(a);
+        if (a.n_pitems + a.n_dctas > 0) fused_cta_scored<DT, D, LAYOUT, false, A><<<dim3(a.n_pitems + a.n_dctas), threads, 0, stream>>>(a);
         break;
     case kLaunchZeroRows:
         if (a.n_zero_rows > 0)

@@ -634,7 +634,7 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         // in the units: 8 requests of 400 keys, 32 / 8 heads 9.3 / 8.6, 8 query heads on one K/V head 9.3 / 9.0, 16 of them
         // (64 channels) 9.8 / 10.7; 256 channels with two 14.7 / 14.6, with four 14.8 / 15.1.
         plan.units_merge = group <= kMergeRows && prm.head_dim <= kMergeDim && plan.max_dsplits >= 2 && plan.max_dsplits <= kMergeSplits &&
-                           (int64_t)plan.dunits.size() <= (int64_t)kWavesPerWg * n_cus && !plan.scored &&
+                           (int64_t)plan.dunits.size() <= (int64_t)kWavesPerWg * n_cus &&
                            next_prow - plan.decode_prow0 <= (int64_t)(sizeof(WsHeader::arrived) / sizeof(uint32_t));
         // The first workers to take a decode seat (one per compute unit) start with four fixed
         // units each, the longest ones, and claim nothing for them.  The other units are dealt
@@ -728,6 +728,11 @@ pod_status build_plan(const pod_attn_params &prm, const int32_t *seq_meta, int n
         if (n_items + plan.n_dwgs <= n_cus || (prm.head_dim <= 128 && n_items <= most_items)) rule = kPrefillFirst;
         else if (prm.head_dim > 128 && n_items <= n_cus && plan.n_dwgs == n_cus) rule = kDecodeFirst;
         plan.fixed_roles = rule;
+    }
+    // (The kernel of changed scores that binds by ticket is not built with the merge.)
+    if (plan.scored && !plan.pitems.empty() && plan.fixed_roles == kRolesByTicket) {
+        plan.units_merge = false;
+        plan.unit_splits.clear();
     }
 
     // ---- which occupancy configuration suits the batch (Section 4.2.2) ----------------------

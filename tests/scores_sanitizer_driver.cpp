@@ -69,7 +69,8 @@ int main(int argc, char **argv)
         const pod_status st = pod::build_plan(prm, meta.data(), 256, plan, err, &sc);
         if (st != POD_OK) { require(!err.empty(), "no message", seed); ++n_refused; continue; }
         ++n_ok;
-        require(plan.ranges.size() == 2 * (size_t)n_rows && !plan.units_merge && !plan.heavy_pays, "shape of the plan", seed);
+        require(plan.ranges.size() == 2 * (size_t)n_rows && !plan.heavy_pays &&
+                    (!plan.units_merge || plan.unit_splits.size() == plan.dunits.size()), "shape of the plan", seed);
         for (const pod::PrefillItem &it : plan.pitems) {
             require(it.kv_begin >= 0 && it.kv_begin <= it.kv_end && it.kv_end <= meta[4 * (size_t)it.req + 2], "keys of an item", seed);
             require(it.split == 0 || it.kv_begin % 16 == 0, "a split inside a step", seed);

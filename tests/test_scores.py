@@ -370,6 +370,30 @@ def test_windows_around_the_edges_of_tiles_and_steps(window):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(32, 8, 128, wl.BF16, 16, False), (8, 1, 64, wl.F16, 0, False), (6, 3, 128, wl.F16, 24, True)])
+@pytest.mark.parametrize("prefill", [(), ((40, 300),)])
+def test_units_of_one_round_merge_their_groups(shape, prefill):
+    """Decodes cut into two to eight units each, with and without a chunk beside them, some seeing nothing; called again and
+    again, since the units' counters have to be back at zero."""
+    batch = grid_batch(*shape, prefill=prefill, decode=(400, 390, 1, 512, 300, 450), seed=9)
+    far = 1 << 30
+    for scores in (pod.Scores(logit_cap=4.0), pod.Scores(window=350, slopes=slopes(shape[0])),
+                   pod.Scores(doc_start=[0] * (batch.n_rows - 6) + [far, 100, 0, 7, far, 33])):
+        hidden = poison_unseen(batch, scores)
+        want = reference(hidden, scores)
+        info = check(hidden, scores, want=want)
+        assert 2 <= info.max_decode_splits <= 8 and info.n_decode_units <= 1024
+        dev = hidden.to("cuda:0")
+        attn = pod.HybridAttention(dev, scores=scores)
+        first = attn.forward(dev).clone()
+        for mode in ("fused", "serial", "fused", "streams", "fused_cta", "fused"):
+            again = attn.forward(dev, mode=pod.MODES[mode])
+            torch.cuda.synchronize()
+            assert torch.equal(again, first), mode
+        attn.close()
+
+
+@pytest.mark.gpu
 def test_rows_that_see_nothing_are_zero():
     """Single rows, blocks of rows, whole requests, a whole batch; beside rows that see keys and alone."""
     for shape in (GRID[0], GRID[1], GRID[4]):
