@@ -197,8 +197,9 @@ void       pod_attn_plan_destroy(pod_attn_plan *plan);
  *
  * i.e. a sliding window, documents that do not see each other packed into one request, and a prefix whose tokens everyone
  * in the request sees, from in front as well.  A row with first >= end sees nothing and its result is 0.
- * What a row does not see does not reach its result, be it infinite or NaN, and cache blocks (or parts of them) whose keys
- * no row of the batch sees are not read: their entries in block_table may name no block.  (Visible values that are infinite
+ * What a row does not see does not reach its result, be it infinite or NaN.  Of a request's keys those ahead of the first
+ * and behind the last one that any of its rows sees are not read: entries of block_table for blocks of such keys alone may name
+ * no block (a window's old blocks can be given back).  (Visible values that are infinite
  * make a result infinite or NaN, as their weighted sum does, or NaN where a decode row re-reads them for keys that do not exist.)
  * With POD_MODE_FLAG_NO_COMBINE decode rows that see nothing are not written either.
  */

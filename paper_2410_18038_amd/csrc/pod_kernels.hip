@@ -348,7 +348,8 @@ __device__ __forceinline__ PrefillItem load_item(const PrefillItem *items, int i
     return PrefillItem{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
 }
 
-// A is KernelArgs, or ScoredArgs for the kernels of plans whose scores are changed or masked by more than causality.
+// A is KernelArgs, or ScoredArgs or CappedArgs for the kernels of plans whose scores are changed or masked by more than
+// causality.
 template <int DT, int D, int LAYOUT, class A>
 __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem it,
                                                  unsigned char *smem)
@@ -775,8 +776,6 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
             live = live && j0 + T > wave_minfirst;
             next_live = next_live && j0 + 2 * T > wave_minfirst;
         }
-        // Matrix blocks ask for issue before the other wavefront's softmax: the two then settle into
-        // opposite phases.  (At 256 channels raised priority costs the decode stream more; see the worker.)
         // Capped scores: already so, and relative to `base`, the running maximum before this tile, where no bias follows.
         [[maybe_unused]] bool polynomial = false, capped = false, relative = false;
         [[maybe_unused]] float base = 0.f;
@@ -786,6 +785,8 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
             relative = capped && !a.slopes;
             if (relative && m_run != neg_inf()) base = m_run;
         }
+        // Matrix blocks ask for issue before the other wavefront's softmax: the two then settle into
+        // opposite phases.  (At 256 channels raised priority costs the decode stream more; see the worker.)
         if constexpr (D <= 128) __builtin_amdgcn_s_setprio(3);
         if (CAPPED && capped) scores_capping(cur ^ 1, s_next, s_cur, base);
         else if (next_live) scores(cur ^ 1, s_next, j0 + T); // matrix unit: scores of the next tile
@@ -883,58 +884,58 @@ __device__ __forceinline__ void prefill_item_run(const A &a, const PrefillItem i
                 }
                 if constexpr (D <= 128) __builtin_amdgcn_s_setprio(2);
             } else {
-            v8 pk[NTB][2];
+                v8 pk[NTB][2];
 #pragma unroll
-            for (int tb = 0; tb < NTB; ++tb)
+                for (int tb = 0; tb < NTB; ++tb)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    pk[tb][r >> 3][r & 7] = (typename N::elem)fast_exp2(__builtin_fmaf(s_cur[tb][r], c, -m_use));
-            // O^T += V^T P^T : rows = channels, contraction over the keys in S's own register order.
-            const POD_LDS unsigned char *vb = lds + (2 + cur) * L::kTileBytes;
-            uint32_t v_base = v_rd0;
-            asm("" : "+v"(v_base));               // as for K above
-            // Operation j = (channel block j / (2 NTB), key block (j / 2) % NTB, half j % 2); its V
-            // fragment is two transposing reads.  As for K, the reads are written and pinned two
-            // operations ahead of the matrix instruction that uses them.
-            constexpr int kAheadV = 2, kOpsV = 2 * NTB * MB, kSums = 2 * NTB;
-            auto v_frag = [&](int j) __attribute__((always_inline)) {
-                const POD_LDS unsigned char *vp = vb + (((j >> 1) % NTB) * 32 + 16 * (j & 1)) * L::kRowBytes +
-                                                  (v_base ^ (uint32_t)((cb0 + j / (2 * NTB)) << 6));
-                const s16x4 lo = lds_read_tr(vp);
-                const s16x4 hi = lds_read_tr(vp + 8 * L::kRowBytes);
-                return __builtin_bit_cast(v8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            };
-            u32x4 pw[kSums];
+                    for (int r = 0; r < 16; ++r)
+                        pk[tb][r >> 3][r & 7] = (typename N::elem)fast_exp2(__builtin_fmaf(s_cur[tb][r], c, -m_use));
+                // O^T += V^T P^T : rows = channels, contraction over the keys in S's own register order.
+                const POD_LDS unsigned char *vb = lds + (2 + cur) * L::kTileBytes;
+                uint32_t v_base = v_rd0;
+                asm("" : "+v"(v_base));               // as for K above
+                // Operation j = (channel block j / (2 NTB), key block (j / 2) % NTB, half j % 2); its V
+                // fragment is two transposing reads.  As for K, the reads are written and pinned two
+                // operations ahead of the matrix instruction that uses them.
+                constexpr int kAheadV = 2, kOpsV = 2 * NTB * MB, kSums = 2 * NTB;
+                auto v_frag = [&](int j) __attribute__((always_inline)) {
+                    const POD_LDS unsigned char *vp = vb + (((j >> 1) % NTB) * 32 + 16 * (j & 1)) * L::kRowBytes +
+                                                      (v_base ^ (uint32_t)((cb0 + j / (2 * NTB)) << 6));
+                    const s16x4 lo = lds_read_tr(vp);
+                    const s16x4 hi = lds_read_tr(vp + 8 * L::kRowBytes);
+                    return __builtin_bit_cast(v8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                };
+                u32x4 pw[kSums];
 #pragma unroll
-            for (int j = 0; j < kSums; ++j) {
-                pw[j] = __builtin_bit_cast(u32x4, pk[j >> 1][j & 1]);
-                // Weight sums, over the rounded weights, the ones the PV product uses: a 4x4x4 product with ones
-                // adds four weights of every lane in 8 cycles of the matrix pipe, where a two-element dot
-                // product (which runs in that pipe too) takes 16 for two.  With the issue priority
-                // below, prefill of 8192 tokens 544 -> 528 us, the prefill-heavy configuration at 32K
-                // contexts 1217 -> 1143.
-                asm("" : "+v"(pw[j]));                       // packed once, for both uses
-                l_run = N::add_all(u32x2{pw[j][0], pw[j][1]}, l_run);
-                l_run = N::add_all(u32x2{pw[j][2], pw[j][3]}, l_run);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (D <= 128) __builtin_amdgcn_s_setprio(3);
-            v8 vv[kOpsV];
+                for (int j = 0; j < kSums; ++j) {
+                    pw[j] = __builtin_bit_cast(u32x4, pk[j >> 1][j & 1]);
+                    // Weight sums, over the rounded weights, the ones the PV product uses: a 4x4x4 product with ones
+                    // adds four weights of every lane in 8 cycles of the matrix pipe, where a two-element dot
+                    // product (which runs in that pipe too) takes 16 for two.  With the issue priority
+                    // below, prefill of 8192 tokens 544 -> 528 us, the prefill-heavy configuration at 32K
+                    // contexts 1217 -> 1143.
+                    asm("" : "+v"(pw[j]));                       // packed once, for both uses
+                    l_run = N::add_all(u32x2{pw[j][0], pw[j][1]}, l_run);
+                    l_run = N::add_all(u32x2{pw[j][2], pw[j][3]}, l_run);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (D <= 128) __builtin_amdgcn_s_setprio(3);
+                v8 vv[kOpsV];
 #pragma unroll
-            for (int j = 0; j < kAheadV; ++j) vv[j] = v_frag(j);
+                for (int j = 0; j < kAheadV; ++j) vv[j] = v_frag(j);
 #pragma unroll
-            for (int j = 0; j < kOpsV; ++j) {
-                if (j + kAheadV < kOpsV) vv[j + kAheadV] = v_frag(j + kAheadV);
-                o[j / (2 * NTB)] = N::mfma32(vv[j], __builtin_bit_cast(v8, pw[j % kSums]), o[j / (2 * NTB)]);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAheadV, 0);
+                for (int j = 0; j < kOpsV; ++j) {
+                    if (j + kAheadV < kOpsV) vv[j + kAheadV] = v_frag(j + kAheadV);
+                    o[j / (2 * NTB)] = N::mfma32(vv[j], __builtin_bit_cast(v8, pw[j % kSums]), o[j / (2 * NTB)]);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAheadV, 0);
 #pragma unroll
-            for (int j = 0; j < kOpsV - kAheadV; ++j) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, kAheadV, 0);
-            if constexpr (D <= 128) __builtin_amdgcn_s_setprio(2);
+                for (int j = 0; j < kOpsV - kAheadV; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, kAheadV, 0);
+                if constexpr (D <= 128) __builtin_amdgcn_s_setprio(2);
             }
         }
         wait_all_loads();                                    // K tile jt+2 and V tile jt+1 have landed
