@@ -358,7 +358,8 @@ pod_status pod_attn_forward_static(const void *prefill_q, const void *decode_q,
  * says how many blocks are missing.  A request that cannot be (q_len < 1, kv_len < q_len, a decode with q_len other than
  * 1, cache_row outside the cache, kv_len beyond its row, q_start outside the rows) takes no blocks, and those of its rows
  * that exist get slot -1 and position 0.  A row whose token lies in a block entry outside [0, n_blocks) gets slot -1 as well.
- * Requests that share a cache_row must not need blocks for it, and a free list must not name a block twice.
+ * Requests that share a cache_row must not need blocks for it, and a free list must not name a block twice, or one that the
+ * cache does not have; of a row that two requests name either may be written.
  */
 pod_status pod_attn_build_tables(const pod_attn_params *params, const int32_t *seq_meta, const int32_t *free_blocks,
                                  int32_t n_free, int32_t *block_table, int32_t n_rows, int32_t *slots, int32_t *positions,

@@ -631,8 +631,8 @@ static pod_status cache_slots(const pod_attn_params &prm, int32_t *per_block, in
 {
     const int64_t token_elems = (int64_t)prm.n_kv_heads * prm.head_dim;
     const int64_t per = prm.block_size > 0 ? prm.block_size : prm.kv_seq_stride / token_elems;
-    const int64_t n = per * (prm.block_size > 0 ? prm.n_blocks : prm.n_cache_rows);
     if (per < 1) return fail(POD_ERR_INVALID_ARG, "kv_seq_stride holds no token");
+    const int64_t n = std::min<int64_t>(per, INT64_C(1) << 31) * (prm.block_size > 0 ? prm.n_blocks : prm.n_cache_rows);
     if (per > INT32_MAX || n > INT32_MAX) return fail(POD_ERR_UNSUPPORTED, "the cache has more than 2^31 - 1 slots");
     *per_block = (int32_t)per;
     *n_slots = (int32_t)n;

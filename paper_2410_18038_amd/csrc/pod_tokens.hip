@@ -279,7 +279,7 @@ static hipError_t launch_append_steps(const AppendArgs &a, int layout, hipStream
 {
     constexpr int heads = append_heads(D) * STEPS;
     const int n_heads = a.n_q_heads + 2 * a.n_kv_heads;
-    const dim3 grid((a.n_rows + kWavesPerWg - 1) / kWavesPerWg, (n_heads + heads - 1) / heads), threads(kWgThreads);
+    const dim3 grid(((uint32_t)a.n_rows + kWavesPerWg - 1) / kWavesPerWg, (n_heads + heads - 1) / heads), threads(kWgThreads);
     if (layout == POD_ROPE_HALF) append_tokens<DT, D, POD_ROPE_HALF, STEPS><<<grid, threads, 0, stream>>>(a);
     else append_tokens<DT, D, POD_ROPE_INTERLEAVED, STEPS><<<grid, threads, 0, stream>>>(a);
     return hipGetLastError();
@@ -289,8 +289,8 @@ static hipError_t launch_append_as(const AppendArgs &a, int layout, hipStream_t 
 {
     // One group of heads a wavefront up to a few rounds of the chip, then two, which halves the work on angles.  us at 128
     // channels, 32 / 8 heads, one group / two / four: 16 rows 3.0 / 3.6 / 5.0, 256 rows 3.5 / 4.0 / 5.4, 1024 rows (6144
-    // wavefronts of one group) 6.2 / 6.1 / 7.0; 256 channels, 4096 rows 26.6 / 23.4 / 25.1; 64 channels, 1024 rows (3072)
-    // 4.30 / 4.33 / 5.1, 2048 rows 6.1 / 5.9.
+    // wavefronts of one group) 6.2 / 6.1 / 7.0; 256 channels, 4096 rows 26.6 / 23.4 / 25.1; 64 channels, 1024 rows (half
+    // as many) 4.30 / 4.33 / 5.1, 2048 rows 6.1 / 5.9.
     const int64_t waves = (int64_t)a.n_rows * ((a.n_q_heads + 2 * a.n_kv_heads + append_heads(D) - 1) / append_heads(D));
     return waves < 6 * 1024 ? launch_append_steps<DT, D, 1>(a, layout, stream) : launch_append_steps<DT, D, 2>(a, layout, stream);
 }

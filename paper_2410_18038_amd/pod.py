@@ -254,6 +254,10 @@ def pod_attn_plan_create_scored(params: Params, scores: Optional[Scores], seq_me
     if scores is None:
         _check(lib().pod_attn_plan_create_scored(ctypes.byref(params), None, meta_p, ctypes.byref(handle)))
         return Plan(handle.value, params)
+    if not -2**31 <= scores.window < 2**31:
+        raise ValueError(f"window {scores.window} does not fit in 32 bits")
+    if scores.logit_cap > 0 and not np.float32(scores.logit_cap) > 0:
+        raise ValueError(f"logit_cap {scores.logit_cap} is 0 in 32 bits")
     n_rows = int(meta[:params.n_prefill, 1].clip(min=0).sum()) + params.n_decode
     kept, ptr = [], {}
     for name, size, dtype, ctype in (("slopes", params.n_q_heads, np.float32, ctypes.c_float),
@@ -631,6 +635,10 @@ class HybridAttention:
         attention reads them.  q, k, v: [rows, heads * head_dim] in the order of the output rows; rows behind the batch are
         padding.  The queries of ``batch`` are not read.  Returns the output rows."""
         n = batch.n_rows
+        for name in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "block_size", "kv_order"):
+            mine, given = getattr(self.params, name), (getattr(append.params, name), getattr(tables.params, name))
+            if given != (mine, mine):
+                raise ValueError(f"{name} is {mine} in the plan, {given[0]} in the append, {given[1]} in the tables")
         if q.shape[0] < n:
             raise ValueError(f"{q.shape[0]} rows of projections for a batch of {n}")
         rows = append(q, k, v, tables.slots, tables.positions, batch.k_cache, batch.v_cache)

@@ -203,6 +203,9 @@ def test_score_arguments_are_checked():
     with pytest.raises(pod.PodError) as e:
         plan(pod.Scores(), head_dim=96)
     assert e.value.status == -2
+    for scores in [pod.Scores(window=2**32 + 1), pod.Scores(logit_cap=1e-60)]:           # values that change on their way to 32 bits
+        with pytest.raises(ValueError):
+            plan(scores)
     wide = wl.config_batch(1)
     wide = dataclasses.replace(wide, head_dim=128, softmax_scale=1.0, kv_seq_stride=2 * wide.kv_seq_stride)   # head_dim 128, contiguous: built for the configuration otherwise
     plan = pod.pod_attn_plan_create_scored(plain_params(wide), pod.Scores(logit_cap=5.0), wide.seq_meta)
@@ -551,6 +554,28 @@ def test_capture_static_scratch_and_repeated_calls_give_the_same_bits():
     torch.cuda.synchronize()
     assert torch.equal(out, want)
     attn.close()
+
+
+@pytest.mark.gpu
+def test_plans_on_two_streams_at_once_give_the_bits_of_each_alone():
+    """A plan bound by ticket whose groups a kernel of its own merges, and one of decodes that merge themselves; each has its
+    own workspace, and what one call clears must be the next one's of the same plan only."""
+    runs = []
+    for decode, prefill, name, kw in [((900, 31, 64, 257, 1200), ((200, 333), (37, 37)), "all", dict(decode_chunk=128, prefill_split_len=64, max_prefill_waves=64)),
+                                      ((1500, 700, 1), (), "cap", {})]:
+        batch = grid_batch(8, 2, 128, wl.BF16, 16, False, prefill=prefill, decode=decode)
+        dev = batch.to("cuda:0")
+        attn = pod.HybridAttention(dev, scores=variant(name, batch), **kw)
+        runs.append((dev, attn, attn.forward(dev).clone(), torch.cuda.Stream(), []))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for dev, attn, _, stream, got in runs:
+            with torch.cuda.stream(stream):
+                got.append(attn.forward(dev))
+    torch.cuda.synchronize()
+    for _, attn, want, _, got in runs:
+        assert all(torch.equal(g, want) for g in got)
+        attn.close()
 
 
 @pytest.mark.gpu

@@ -459,6 +459,46 @@ def test_a_table_entry_that_names_no_block_gives_no_slot():
 
 
 # -- together ------------------------------------------------------------------------------------- #
+def test_a_layer_refuses_calls_made_for_another_shape():
+    """Rows of other heads, another type or another cache would be read as if they were the plan's."""
+    mine = make_params()
+    attn = pod.HybridAttention.__new__(pod.HybridAttention)
+    attn.params = mine
+    batch = wl.make_batch("other", prefill=[], decode_kv_lens=[5], n_q_heads=8, n_kv_heads=2, head_dim=128, dtype=wl.BF16, seed=1)
+    q = k = v = torch.zeros(1, 8)
+    for other in [dict(hq=4), dict(hkv=1), dict(d=64), dict(dtype=wl.F16), dict(block=0), dict(head_major=True)]:
+        theirs = make_params(**other)
+        for a, t in [(theirs, mine), (mine, theirs)]:
+            with pytest.raises(ValueError, match="in the plan"):
+                attn.forward_tokens(batch, pod.TokenAppend(a, device="cpu"), pod.TokenTables(t, 4, device="cpu"), q, k, v)
+
+
+@pytest.mark.gpu
+def test_token_calls_follow_the_current_stream():
+    """Inputs that a stream is still writing, read by calls on it: only calls on another stream could see them too early."""
+    batch = wl.make_batch("side", prefill=[(50, 333)], decode_kv_lens=[700, 31, 257], n_q_heads=4, n_kv_heads=4, head_dim=64,
+                          dtype=wl.F16, seed=42, block_size=0, max_len=704).to("cuda:0")
+    attn = pod.HybridAttention(batch)
+    tables, append = pod.TokenTables(attn.params, batch.n_rows), pod.TokenAppend(attn.params, rope=pod.Rope(64))
+    qkv = torch.randn(batch.n_rows, 12 * 64, device="cuda:0").half()
+    layer = lambda meta, x: attn.forward_tokens(batch, append, tables.build(meta), x[:, :256], x[:, 256:512], x[:, 512:])
+    want = layer(attn.seq_meta_dev, qkv).clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        meta, late = torch.zeros_like(attn.seq_meta_dev), torch.zeros_like(qkv)
+        tables.slots.fill_(-1)
+        busy = torch.randn(4096, 4096, device="cuda:0")
+        for _ in range(4):
+            busy = (busy @ busy).tanh()
+        meta.copy_(attn.seq_meta_dev)
+        late.copy_(qkv)
+        got = layer(meta, late)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    attn.close()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("block,head_major", [(16, False), (24, False), (0, False), (64, True)])
 def test_a_layer_from_its_projections(block, head_major):
