@@ -543,6 +543,7 @@ class TokenAppend:
     def __init__(self, params: Params, *, rope: Optional[Rope] = None, norm: Optional[HeadNorm] = None, device="cuda"):
         import torch
         self.params, self.device = params, _device(device)
+        self.index = self.device.index if self.device.type == "cuda" else -1
         self.dtype = {F16: torch.float16, BF16: torch.bfloat16}[params.dtype]
         self.rope, self.table, self.norm = None, None, None
         if rope is not None:
@@ -560,27 +561,40 @@ class TokenAppend:
         p = params
         n, tokens = (p.n_blocks, p.block_size) if p.block_size > 0 else (p.n_cache_rows, p.kv_seq_stride // max(p.n_kv_heads * p.head_dim, 1))
         self.cache_shape = (n, p.n_kv_heads, tokens, p.head_dim) if p.kv_order == KV_HEAD_MAJOR else (n, tokens, p.n_kv_heads, p.head_dim)
+        self._rows = p.n_q_heads * p.head_dim, p.n_kv_heads * p.head_dim, p.n_q_heads, p.head_dim
         ref = lambda x: None if x is None else ctypes.byref(x)
         self._args = ref(params), ref(self.rope), 0 if self.table is None else self.table.data_ptr(), ref(self.norm)
 
     def __call__(self, q, k, v, slots, positions, k_cache, v_cache, q_out=None):
         """q, k, v: [rows, heads * head_dim] (or views of one projection); returns q_out, [rows, Hq, d]."""
         import torch
-        p, dev, dtype, rows = self.params, self.device, self.dtype, slots.shape[0]
-        q_row, kv_row = p.n_q_heads * p.head_dim, p.n_kv_heads * p.head_dim
-        _need(q, "q", dtype, (rows, q_row), dev, strided=True)
-        _need(k, "k", dtype, (rows, kv_row), dev, strided=True)
-        _need(v, "v", dtype, (rows, kv_row), dev, strided=True)
-        _need(slots, "slots", torch.int32, (rows,), dev)
-        _need(positions, "positions", torch.int32, (rows,), dev)
-        _need(k_cache, "k_cache", dtype, self.cache_shape, dev)
-        _need(v_cache, "v_cache", dtype, self.cache_shape, dev)
+        dev, dtype, i, i32 = self.device, self.dtype, self.index, torch.int32
+        q_row, kv_row, heads, d = self._rows
+        flat = slots.shape
+        rows = flat[0] if flat else 0
         if q_out is None:
-            q_out = torch.empty((rows, p.n_q_heads, p.head_dim), dtype=dtype, device=dev)
-        else:
-            _need(q_out, "q_out", dtype, (rows, p.n_q_heads, p.head_dim), dev)
+            q_out = torch.empty((rows, heads, d), dtype=dtype, device=dev)
+        kv_shape, cache_shape, q_strides, k_strides, v_strides = (rows, kv_row), self.cache_shape, q.stride(), k.stride(), v.stride()
+        # What _need asks of each tensor, written out: a decode step of few rows waits for this call (8 of its 8.7 us with a call of
+        # _need for each).  Where something does not fit, _need says what.
+        if not (q.dtype is dtype and k.dtype is dtype and v.dtype is dtype and k_cache.dtype is dtype and v_cache.dtype is dtype and
+                q_out.dtype is dtype and slots.dtype is i32 and positions.dtype is i32 and
+                q.shape == (rows, q_row) and k.shape == kv_shape and v.shape == kv_shape and k_cache.shape == cache_shape and
+                v_cache.shape == cache_shape and q_out.shape == (rows, heads, d) and len(flat) == 1 and positions.shape == flat and
+                q.get_device() == i and k.get_device() == i and v.get_device() == i and k_cache.get_device() == i and
+                v_cache.get_device() == i and q_out.get_device() == i and slots.get_device() == i and positions.get_device() == i and
+                q_strides[1] == 1 and k_strides[1] == 1 and v_strides[1] == 1 and k_cache.is_contiguous() and
+                v_cache.is_contiguous() and q_out.is_contiguous() and slots.is_contiguous() and positions.is_contiguous()):
+            _need(slots, "slots", i32, (rows,), dev)
+            _need(positions, "positions", i32, (rows,), dev)
+            _need(q, "q", dtype, (rows, q_row), dev, strided=True)
+            _need(k, "k", dtype, kv_shape, dev, strided=True)
+            _need(v, "v", dtype, kv_shape, dev, strided=True)
+            _need(k_cache, "k_cache", dtype, cache_shape, dev)
+            _need(v_cache, "v_cache", dtype, cache_shape, dev)
+            _need(q_out, "q_out", dtype, (rows, heads, d), dev)
         # (a single row has no distance to a next one: torch may name any)
-        q_stride, k_stride, v_stride = (q.stride(0), k.stride(0), v.stride(0)) if rows > 1 else (q_row, kv_row, kv_row)
+        q_stride, k_stride, v_stride = (q_strides[0], k_strides[0], v_strides[0]) if rows > 1 else (q_row, kv_row, kv_row)
         ref, rope, table, norm = self._args
         _call(dev, lib().pod_attn_append, ref, rope, table, norm, q.data_ptr(), q_stride, k.data_ptr(), k_stride, v.data_ptr(),
               v_stride, slots.data_ptr(), positions.data_ptr(), rows, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
