@@ -58,25 +58,33 @@ __device__ __forceinline__ int64_t wave_sum(int64_t x)
 __global__ __launch_bounds__(kWgThreads) void token_tables(TableArgs a)
 {
     __shared__ int64_t part[kWavesPerWg][4];
+    __shared__ int ends[kWavesPerWg];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n_req = a.n_prefill + a.n_decode;
     const int b = (int)blockIdx.x;
     const bool decode_wg = b < a.n_decode_wgs;
     const int prefill_req = decode_wg ? -1 : (b - a.n_decode_wgs) / max(a.wgs_per_prefill, 1);
     const int first_req = decode_wg ? a.n_prefill + b * kWgThreads : prefill_req;    // the workgroup's (first) request
-    // blocks of the requests before that, of all, prefill rows, refused requests
+    // blocks of the requests before that, of all, prefill rows, refused requests; and the row behind the last prefill row
     int64_t before = 0, total = 0, prows = 0, refused = 0;
+    int end = 0;
     for (int r = tid; r < n_req; r += kWgThreads) {
         const Request x = read_request(a, r);
         total += x.fresh;
         before += r < first_req ? x.fresh : 0;
         prows += r < a.n_prefill ? max(x.q_len, 0) : 0;
+        end = r < a.n_prefill && x.ok ? max(end, x.start + x.q_len) : end;
         refused += x.ok ? 0 : 1;
     }
     before = wave_sum(before); total = wave_sum(total); prows = wave_sum(prows); refused = wave_sum(refused);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) end = max(end, __shfl_xor(end, d));
+    if (lane == 0) ends[wave] = end;
     if (lane == 0) { part[wave][0] = before; part[wave][1] = total; part[wave][2] = prows; part[wave][3] = refused; }
     __syncthreads();
     before = total = prows = refused = 0;
+#pragma unroll
+    for (int w = 0; w < kWavesPerWg; ++w) end = max(end, ends[w]);
 #pragma unroll
     for (int w = 0; w < kWavesPerWg; ++w) { before += part[w][0]; total += part[w][1]; prows += part[w][2]; refused += part[w][3]; }
     const bool enough = total <= a.n_free;
@@ -87,8 +95,15 @@ __global__ __launch_bounds__(kWgThreads) void token_tables(TableArgs a)
         a.report[2] = (int32_t)refused;
         a.report[3] = (int32_t)min(covered, (int64_t)0x7fffffff);
     }
-    // padding rows, dealt over the whole launch
+    // Padding rows, dealt over the whole launch.  (Where a request is refused or rows leave a gap, rows of other requests may
+    // lie behind as many rows as there are; those are theirs.)
     for (int64_t i = covered + (int64_t)b * kWgThreads + tid; i < a.n_rows; i += (int64_t)gridDim.x * kWgThreads) {
+        bool taken = false;
+        for (int r = 0; r < a.n_prefill && i < end; ++r) {
+            const Request x = read_request(a, r);
+            taken |= x.ok && i >= x.start && i - x.start < x.q_len;
+        }
+        if (taken) continue;
         a.slots[i] = -1;
         a.positions[i] = 0;
     }

@@ -425,6 +425,18 @@ def test_requests_that_cannot_be_are_refused_and_the_others_served():
         assert tables.report.tolist()[2] == 1
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("column,value", [(0, 5000), (1, 0), (1, -40)])
+def test_rows_behind_a_gap_are_no_padding(column, value):
+    """The second request begins behind as many rows as the batch has: they are its rows, and those around them padding."""
+    meta, table, free, n_blocks, n_rows = make_tables([(3000, 3000), (2500, 2600)], [17], 16, seed=16, pad=6000)
+    meta[1 if column == 0 else 0, column] = value
+    for _ in range(5):
+        tables = run_refused(meta, 2, 1, 16, table, free, n_blocks, n_rows, len(meta))
+        placed, last = (5500, 7500) if column == 0 else (2501, 5500)      # (with a gap the decode row is one of the second request's)
+        assert int((tables.slots >= 0).sum()) == placed and bool((tables.slots[last:] == -1).all())
+
+
 def run_refused(meta, n_prefill, n_decode, block, table, free, n_blocks, n_rows, n_cache_rows):
     """Like run_tables, but only the rows that exactly one request names are compared."""
     prm = make_params(n_prefill=n_prefill, n_decode=n_decode, block=block, n_blocks=n_blocks, rows=n_cache_rows, max_blocks=table.shape[1])
