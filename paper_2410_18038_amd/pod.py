@@ -482,6 +482,14 @@ def _device(device):
     return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
 
 
+_KIND = ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "block_size", "kv_order")
+
+
+def _kind(p: Params):
+    """What the calls of one layer have to have in common, as _KIND names it."""
+    return p.dtype, p.n_q_heads, p.n_kv_heads, p.head_dim, p.block_size, p.kv_order
+
+
 class Rope:
     """Rotary positions: which channels turn together, how fast, and how that is stretched for long contexts.
 
@@ -514,7 +522,7 @@ class TokenTables:
 
     def __init__(self, params: Params, n_rows: int, *, device="cuda"):
         import torch
-        self.params, self.n_rows, self.device = params, int(n_rows), _device(device)
+        self.params, self.n_rows, self.device, self.kind = params, int(n_rows), _device(device), _kind(params)
         self.slots = torch.empty(self.n_rows, dtype=torch.int32, device=self.device)
         self.positions = torch.empty(self.n_rows, dtype=torch.int32, device=self.device)
         self.report = torch.zeros(4, dtype=torch.int32, device=self.device)
@@ -543,7 +551,7 @@ class TokenAppend:
     def __init__(self, params: Params, *, rope: Optional[Rope] = None, norm: Optional[HeadNorm] = None, device="cuda"):
         import torch
         self.params, self.device = params, _device(device)
-        self.index = self.device.index if self.device.type == "cuda" else -1
+        self.index, self.kind = self.device.index if self.device.type == "cuda" else -1, _kind(params)
         self.dtype = {F16: torch.float16, BF16: torch.bfloat16}[params.dtype]
         self.rope, self.table, self.norm = None, None, None
         if rope is not None:
@@ -633,15 +641,19 @@ class HybridAttention:
         pod_attn_plan_upload(self.plan, self.ws_ptr, self.ws_bytes, stream)
 
     def forward(self, batch, out=None, mode=MODE_FUSED):
+        ptr = lambda t: 0 if t is None else t.data_ptr()                   # (0 of an empty tensor)
+        return self._forward(ptr(batch.prefill_q), ptr(batch.decode_q), batch, out, mode)
+
+    def _forward(self, prefill_q, decode_q, batch, out, mode):
         torch = self.torch
         dev = batch.k_cache.device
         if out is None:
             out = torch.empty((batch.n_rows, batch.n_q_heads, batch.head_dim), dtype=batch.torch_dtype,
                               device=dev)
-        ptr = lambda t: 0 if t is None or t.numel() == 0 else t.data_ptr()
-        _call(dev, lib().pod_attn_forward, ptr(batch.prefill_q), ptr(batch.decode_q), ptr(batch.k_cache), ptr(batch.v_cache),
-              self.seq_meta_dev.data_ptr(), ptr(batch.block_table), out.data_ptr(), self.plan.handle, self.ws_ptr, self.ws_bytes,
-              mode, _stream_of(dev))
+        table = batch.block_table
+        _call(dev, lib().pod_attn_forward, prefill_q, decode_q, batch.k_cache.data_ptr(), batch.v_cache.data_ptr(),
+              self.seq_meta_dev.data_ptr(), 0 if table is None else table.data_ptr(), out.data_ptr(), self.plan.handle,
+              self.ws_ptr, self.ws_bytes, mode, _stream_of(dev))
         return out
 
     def forward_tokens(self, batch, append: TokenAppend, tables: TokenTables, q, k, v, out=None, mode=MODE_FUSED):
@@ -649,15 +661,15 @@ class HybridAttention:
         attention reads them.  q, k, v: [rows, heads * head_dim] in the order of the output rows; rows behind the batch are
         padding.  The queries of ``batch`` are not read.  Returns the output rows."""
         n = batch.n_rows
-        for name in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "block_size", "kv_order"):
-            mine, given = getattr(self.params, name), (getattr(append.params, name), getattr(tables.params, name))
-            if given != (mine, mine):
-                raise ValueError(f"{name} is {mine} in the plan, {given[0]} in the append, {given[1]} in the tables")
+        kind = _kind(self.params)
+        if append.kind != kind or tables.kind != kind:
+            differing = [name for name, *of in zip(_KIND, kind, append.kind, tables.kind) if len(set(of)) > 1]
+            raise ValueError(f"{', '.join(differing)} in the plan, {kind}, differ from those of the append, {append.kind}, or the tables, {tables.kind}")
         if q.shape[0] < n:
             raise ValueError(f"{q.shape[0]} rows of projections for a batch of {n}")
         rows = append(q, k, v, tables.slots, tables.positions, batch.k_cache, batch.v_cache)
-        batch = dataclasses.replace(batch, prefill_q=rows[:batch.n_prefill_rows], decode_q=rows[batch.n_prefill_rows:n])
-        return self.forward(batch, out=out, mode=mode)
+        first = rows.data_ptr()
+        return self._forward(first, first + batch.n_prefill_rows * rows.stride(0) * rows.element_size(), batch, out, mode)
 
     def enable_trace(self):
         """Allocate a trace buffer (one record per workgroup) and switch tracing on."""
