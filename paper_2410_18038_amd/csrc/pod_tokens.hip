@@ -25,8 +25,7 @@ __device__ __forceinline__ int divide(int t, int divisor, uint32_t magic, int &r
 // (exclusive prefix sum: request r takes free_blocks[before_r ..]) and of the whole batch (does the list hold enough?)
 // from the request lengths themselves, 16 bytes a request that every workgroup finds in its L2, and then writes its own
 // rows.  What bounds it is the launch and two dependent round trips (256 decodes 3.4 us, 6 prompts and 500 decodes, 27K rows,
-// 4.6).  A decode request is a thread; the tokens of a
-// prefill request are dealt to several workgroups.
+// 4.7).  A decode request is a thread; the tokens of a prefill request are dealt to several workgroups.
 // ------------------------------------------------------------------------------------------
 struct Request { int start, q_len, kv_len, row, held, fresh; bool ok; };
 
