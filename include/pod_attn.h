@@ -336,7 +336,7 @@ pod_status pod_attn_forward_static(const void *prefill_q, const void *decode_q,
  * looked at), launch one kernel on `stream`, keep no state, allocate nothing and may be recorded into a graph.
  *
  * A slot names a token's place in the cache: for a paged cache block * block_size + offset, for a contiguous one
- * cache_row * max_len + token with max_len = kv_seq_stride / (n_kv_heads * head_dim).  Rows are the rows of `out` of the
+ * cache_row * max_len + token with max_len = kv_seq_stride / (n_kv_heads * head_dim), rounded down.  Rows are the rows of `out` of the
  * attention call: prefill rows first, then a row per decode request; rows behind them are padding (a batch padded to the
  * size of a captured graph).
  */

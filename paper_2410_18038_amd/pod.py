@@ -461,10 +461,15 @@ def _call(device, function, *args):
         _check(status)
 
 
-def _need(t, what, dtype, shape, device, strided=False):
+def _apart(t, strides):
+    """Whether the elements of t lie this far apart in each dimension (one of size 1 has no next element)."""
+    return all(n == 1 or is_ == ought for n, is_, ought in zip(t.shape, t.stride(), strides))
+
+
+def _need(t, what, dtype, shape, device, strided=False, strides=None):
     """Raises ValueError unless t is a tensor of this type and shape on this device, in one piece (with `strided`, of two
-    dimensions, whose rows are).  A None in the shape is any size."""
-    if t.dtype is dtype and t.shape == shape and t.device == device and (t.stride(1) == 1 if strided else t.is_contiguous()):
+    dimensions, whose rows are; with `strides`, with elements that far apart).  A None in the shape is any size."""
+    if t.dtype is dtype and t.shape == shape and t.device == device and strides is None and (t.stride(1) == 1 if strided else t.is_contiguous()):
         return
     if t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
@@ -472,6 +477,10 @@ def _need(t, what, dtype, shape, device, strided=False):
         raise ValueError(f"{what} must be on {device}, not {t.device}")
     if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
         raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if strides is not None:
+        if not _apart(t, strides):
+            raise ValueError(f"{what} must have the strides {tuple(strides)}, not {tuple(t.stride())}")
+        return
     if not (t.is_contiguous() or (strided and t.stride(1) == 1)):
         raise ValueError(f"{what} must lie in one piece" + (" row by row" if strided else ""))
 
@@ -569,15 +578,20 @@ class TokenAppend:
         p = params
         n, tokens = (p.n_blocks, p.block_size) if p.block_size > 0 else (p.n_cache_rows, p.kv_seq_stride // max(p.n_kv_heads * p.head_dim, 1))
         self.cache_shape = (n, p.n_kv_heads, tokens, p.head_dim) if p.kv_order == KV_HEAD_MAJOR else (n, tokens, p.n_kv_heads, p.head_dim)
+        # Rows of a contiguous cache may lie further apart than their tokens; such a cache is a view with gaps.
+        row, stride = p.n_kv_heads * p.head_dim, int(p.kv_seq_stride)
+        self.cache_strides = (stride, row, p.head_dim, 1) if p.block_size <= 0 and stride != tokens * row else None
         self._rows = p.n_q_heads * p.head_dim, p.n_kv_heads * p.head_dim, p.n_q_heads, p.head_dim
         ref = lambda x: None if x is None else ctypes.byref(x)
         self._args = ref(params), ref(self.rope), 0 if self.table is None else self.table.data_ptr(), ref(self.norm)
 
     def __call__(self, q, k, v, slots, positions, k_cache, v_cache, q_out=None):
-        """q, k, v: [rows, heads * head_dim] (or views of one projection); returns q_out, [rows, Hq, d]."""
+        """q, k, v: [rows, heads * head_dim] (or views of one projection); returns q_out, [rows, Hq, d].  The caches are in one
+        piece, or, where kv_seq_stride is no whole number of tokens, views whose rows lie kv_seq_stride elements apart."""
         import torch
         dev, dtype, i, i32 = self.device, self.dtype, self.index, torch.int32
         q_row, kv_row, heads, d = self._rows
+        cache_strides = self.cache_strides
         flat = slots.shape
         rows = flat[0] if flat else 0
         if q_out is None:
@@ -591,15 +605,15 @@ class TokenAppend:
                 v_cache.shape == cache_shape and q_out.shape == (rows, heads, d) and len(flat) == 1 and positions.shape == flat and
                 q.get_device() == i and k.get_device() == i and v.get_device() == i and k_cache.get_device() == i and
                 v_cache.get_device() == i and q_out.get_device() == i and slots.get_device() == i and positions.get_device() == i and
-                q_strides[1] == 1 and k_strides[1] == 1 and v_strides[1] == 1 and k_cache.is_contiguous() and
-                v_cache.is_contiguous() and q_out.is_contiguous() and slots.is_contiguous() and positions.is_contiguous()):
+                q_strides[1] == 1 and k_strides[1] == 1 and v_strides[1] == 1 and cache_strides is None and
+                k_cache.is_contiguous() and v_cache.is_contiguous() and q_out.is_contiguous() and slots.is_contiguous() and positions.is_contiguous()):
             _need(slots, "slots", i32, (rows,), dev)
             _need(positions, "positions", i32, (rows,), dev)
             _need(q, "q", dtype, (rows, q_row), dev, strided=True)
             _need(k, "k", dtype, kv_shape, dev, strided=True)
             _need(v, "v", dtype, kv_shape, dev, strided=True)
-            _need(k_cache, "k_cache", dtype, cache_shape, dev)
-            _need(v_cache, "v_cache", dtype, cache_shape, dev)
+            _need(k_cache, "k_cache", dtype, cache_shape, dev, strides=cache_strides)
+            _need(v_cache, "v_cache", dtype, cache_shape, dev, strides=cache_strides)
             _need(q_out, "q_out", dtype, (rows, heads, d), dev)
         # (a single row has no distance to a next one: torch may name any)
         q_stride, k_stride, v_stride = (q_strides[0], k_strides[0], v_strides[0]) if rows > 1 else (q_row, kv_row, kv_row)

@@ -616,3 +616,89 @@ def test_tensors_that_do_not_fit_are_refused():
     for bad in [(meta[:1], free, table), (meta.long(), free, table), (meta, free, table[:, :4]), (meta.cpu(), free, table)]:
         with pytest.raises(ValueError):
             tables.build(*bad)
+
+
+# -- contiguous caches whose rows lie further apart than their tokens --------------------------------- #
+def gapped_params(rows=5, tokens=40, gap=72, hq=4, hkv=2, d=64, dtype=wl.F16):
+    """Rows of 40 tokens and 72 elements, which are no whole token."""
+    return pod.make_params(n_prefill=0, n_decode=rows, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, dtype=dtype, softmax_scale=1.0,
+                           n_cache_rows=rows, kv_seq_stride=tokens * hkv * d + gap, n_compute_units=256)
+
+
+def gapped_cache(rows=5, tokens=40, gap=72, hkv=2, d=64, **kw):
+    whole = torch.full((rows, tokens * hkv * d + gap), float("nan"), dtype=torch.float16, **kw)
+    return whole, whole[:, :tokens * hkv * d].view(rows, tokens, hkv, d)
+
+
+def test_caches_whose_rows_lie_apart_are_taken_as_such_and_no_others(monkeypatch):
+    """A dense tensor of a cache's shape ends before the last rows that kv_seq_stride names: written as one, the memory behind it."""
+    calls = []
+    monkeypatch.setattr(pod, "_call", lambda device, function, *args: calls.append(args))
+    monkeypatch.setattr(pod, "_stream_of", lambda device: 0)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)
+    for rows in (5, 1):
+        append = pod.TokenAppend(gapped_params(rows=rows), device="cpu")
+        q, k, v = torch.zeros(3, 256).half(), torch.zeros(3, 128).half(), torch.zeros(3, 128).half()
+        whole, apart = gapped_cache(rows=rows)
+        dense = apart.contiguous()
+        append(q, k, v, i32(3), i32(3), apart, apart)
+        assert calls.pop()[14:16] == (whole.data_ptr(), whole.data_ptr())
+        for caches in ((dense, apart), (apart, dense), (dense, dense)):
+            if rows == 1:                                                # the only row has none behind it
+                append(q, k, v, i32(3), i32(3), *caches)
+                calls.pop()
+                continue
+            with pytest.raises(ValueError, match="strides"):
+                append(q, k, v, i32(3), i32(3), *caches)
+    packed = pod.TokenAppend(make_params(hq=4, d=64, dtype=wl.F16, block=0, rows=5, max_len=40), device="cpu")
+    with pytest.raises(ValueError, match="one piece"):
+        packed(torch.zeros(3, 256).half(), torch.zeros(3, 128).half(), torch.zeros(3, 128).half(), i32(3), i32(3), gapped_cache()[1], gapped_cache()[1])
+    assert calls == []
+
+
+@pytest.mark.gpu
+def test_append_to_a_cache_whose_rows_lie_apart():
+    """Every token where its slot names it, nothing between the rows, and the attention reads the same places."""
+    prm = gapped_params()
+    whole, k_cache = gapped_cache(device="cuda:0")
+    whole_v, v_cache = gapped_cache(device="cuda:0")
+    append = pod.TokenAppend(prm)
+    gen = torch.Generator().manual_seed(2)
+    slots = torch.randperm(200, generator=gen)[:90].to(torch.int32)
+    q, k, v = (torch.randn(90, n, generator=gen).half().cuda() for n in (256, 128, 128))
+    q_out = append(q, k, v, slots.cuda(), torch.zeros(90, dtype=torch.int32, device="cuda:0"), k_cache, v_cache)
+    assert torch.equal(q_out.view(90, 256), q)
+    for cache, new, memory in ((k_cache, k, whole), (v_cache, v, whole_v)):
+        want = torch.full((200, 128), float("nan"), dtype=torch.float16)
+        want[slots.long()] = new.cpu()
+        got = cache.reshape(200, 128).cpu()
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+        assert torch.isnan(memory[:, 5120:]).all()
+
+
+@pytest.mark.gpu
+def test_a_layer_over_a_cache_whose_rows_lie_apart():
+    """The same batch and projections over a cache in one piece and over one with gaps: the same bits."""
+    import dataclasses
+    batch = wl.make_batch("apart", prefill=[(50, 333)], decode_kv_lens=[700, 31, 257], n_q_heads=4, n_kv_heads=2, head_dim=64,
+                          dtype=wl.F16, seed=43, block_size=0, max_len=704).to("cuda:0")
+    stride = batch.kv_seq_stride + 40
+    qkv = torch.randn(batch.n_rows, 8 * 64, generator=torch.Generator().manual_seed(4)).half().cuda()
+
+    def layer(b):
+        attn = pod.HybridAttention(b)
+        tables, append = pod.TokenTables(attn.params, b.n_rows).build(attn.seq_meta_dev), pod.TokenAppend(attn.params, rope=pod.Rope(64))
+        out = attn.forward_tokens(b, append, tables, qkv[:, :256], qkv[:, 256:384], qkv[:, 384:])
+        torch.cuda.synchronize()
+        attn.close()
+        return out
+
+    def spread(cache):
+        whole = torch.full((4, stride), float("nan"), dtype=torch.float16, device="cuda:0")
+        whole[:, :batch.kv_seq_stride] = cache.reshape(4, -1)
+        return whole[:, :batch.kv_seq_stride].view(cache.shape)
+
+    other = dataclasses.replace(batch, kv_seq_stride=stride, k_cache=spread(batch.k_cache), v_cache=spread(batch.v_cache))
+    want = layer(batch)
+    got = layer(other)
+    assert torch.equal(got, want) and torch.equal(other.k_cache, batch.k_cache) and torch.equal(other.v_cache, batch.v_cache)
