@@ -351,15 +351,15 @@ pod_status pod_attn_forward_static(const void *prefill_q, const void *decode_q,
  *   free_blocks  device, int32 [n_free]; NULL for a contiguous cache (then n_free = 0)
  *   block_table  device, int32 [n_cache_rows][max_blocks_per_seq], read and written; NULL for a contiguous cache
  *   slots,       device, int32 [n_rows] each: slot and position of every row.  n_rows is at least the batch's rows; padding
- *   positions    rows get slot -1 and position 0.  A row that is no row of `out` because prefill rows leave a gap, or decode
- *                rows a q_start out, is not written.
+ *   positions    rows get slot -1 and position 0, and so does a row that is no row of `out` because prefill rows leave a
+ *                gap, or decode rows a q_start out.
  *   report       device, int32 [4]: blocks taken, blocks missing, requests refused, rows of the batch
  * With fewer free blocks than the batch needs nothing is taken: block_table is left as it is, every slot is -1 and report
  * says how many blocks are missing.  A request that cannot be (q_len < 1, kv_len < q_len, a decode with q_len other than
  * 1, cache_row outside the cache, kv_len beyond its row, q_start outside the rows) takes no blocks, and those of its rows
- * that exist get slot -1 and position 0.  A row whose token lies in a block entry outside [0, n_blocks) gets slot -1 as well.
+ * that exist and are no other request's get slot -1 and position 0.  A row whose token lies in a block entry outside [0, n_blocks) gets slot -1 as well.
  * Requests that share a cache_row must not need blocks for it, and a free list must not name a block twice, or one that the
- * cache does not have; of a row that two requests name either may be written.
+ * cache does not have; of a row that two accepted requests name either may be written.
  */
 pod_status pod_attn_build_tables(const pod_attn_params *params, const int32_t *seq_meta, const int32_t *free_blocks,
                                  int32_t n_free, int32_t *block_table, int32_t n_rows, int32_t *slots, int32_t *positions,

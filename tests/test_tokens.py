@@ -702,3 +702,90 @@ def test_a_layer_over_a_cache_whose_rows_lie_apart():
     want = layer(batch)
     got = layer(other)
     assert torch.equal(got, want) and torch.equal(other.k_cache, batch.k_cache) and torch.equal(other.v_cache, batch.v_cache)
+
+
+# -- rows that no request owns ------------------------------------------------------------------------- #
+def owned_rows_reference(meta, n_prefill, n_decode, block, n_free, free, table, n_rows, n_cache_rows, n_blocks):
+    """(slots, positions, how many accepted requests own the row, table): a row without an owner has slot -1 and position 0."""
+    per_row, table = table.shape[1] * block, table.copy()
+    slots, positions, owners = np.full(n_rows, -1, np.int64), np.zeros(n_rows, np.int64), np.zeros(n_rows, np.int64)
+    prows = sum(max(int(m[1]), 0) for m in meta[:n_prefill])
+    blocks = lambda n: -(-n // block)
+    accepted = []
+    for r, (start, q, kv, row) in enumerate(meta.tolist()):
+        at = start + (prows if r >= n_prefill else 0)
+        if (q >= 1 and kv >= q and start >= 0 and 0 <= row < n_cache_rows and kv <= per_row and
+                (start + q <= n_rows if r < n_prefill else q == 1 and start < n_decode)):
+            accepted.append((at, q, kv, row))
+    enough, taken = sum(blocks(kv) - blocks(kv - q) for _, q, kv, _ in accepted) <= n_free, 0
+    for at, q, kv, row in accepted:
+        held, need = blocks(kv - q), blocks(kv)
+        if enough:
+            table[row, held:need] = free[taken:taken + need - held]
+            taken += need - held
+        inside = max(0, min(q, n_rows - at))                             # (only decode rows can lie behind the last one)
+        pos = np.arange(kv - q, kv)[:inside]
+        entry = table[row, pos // block]
+        owners[at:at + inside] += 1
+        positions[at:at + inside] = pos
+        slots[at:at + inside] = np.where(enough & (entry >= 0) & (entry < n_blocks), entry * block + pos % block, -1)
+    return slots, positions, owners, table
+
+
+ORDERS = {   # what becomes of (q_start, q_len, kv_len, cache_row) of three prompts, 40, 20 and 33 tokens, and four decodes
+    "as they come": {}, "another order": {(0, 0): 53, (1, 0): 33, (2, 0): 0}, "a gap": {(2, 0): 63}, "a gap at the front": {(0, 0): 100},
+    "over each other": {(1, 0): 39, (2, 0): 65}, "as far as without a gap": {(1, 0): 0},
+    "begins before the rows": {(0, 0): -7}, "ends behind them": {(2, 0): 90}, "no tokens": {(1, 1): 0}, "fewer than none": {(0, 1): -3},
+    "more than its context": {(0, 2): 39}, "no such cache row": {(2, 3): 99}, "longer than its cache row": {(1, 2): 1 << 30},
+    "a decode before the rows": {(4, 0): -1}, "a decode behind them": {(3, 0): 9}, "the same row twice": {(5, 0): 1}, "none left": {(3, 0): 9, (4, 0): -2, (5, 0): 9, (6, 1): 2},
+    "a refused prompt over one that is not": {(1, 0): 0, (1, 2): 5}, "a refused decode's row": {(3, 3): 99}, "a decode of two tokens": {(6, 1): 2}}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ORDERS)
+@pytest.mark.parametrize("short", [False, True])
+def test_rows_that_no_request_owns_get_no_slot(name, short):
+    """A slot left by the batch before would have the append write over a token that is still in use."""
+    meta, table, free, n_blocks, n_rows = make_tables([(40, 50), (20, 20), (33, 90)], [17, 1, 32, 48], 16, seed=17, pad=20, missing=1 if short else 0)
+    meta[3:, 0] = [0, 2, 1, 3]
+    for (request, column), value in ORDERS[name].items():
+        meta[request, column] = value
+    prm = make_params(n_prefill=3, n_decode=4, block=16, n_blocks=n_blocks, rows=len(meta), max_blocks=table.shape[1])
+    tables = pod.TokenTables(prm, n_rows)
+    tables.slots.fill_(5)
+    tables.positions.fill_(77)
+    dev_table = torch.from_numpy(table).cuda()
+    tables.build(torch.from_numpy(meta).cuda(), torch.from_numpy(free).cuda(), dev_table)
+    slots, positions, owners, want_table = owned_rows_reference(meta, 3, 4, 16, len(free), free, table, n_rows, len(meta), n_blocks)
+    once = owners <= 1
+    assert tables.slots.cpu().numpy()[once].tolist() == slots[once].tolist()
+    assert tables.positions.cpu().numpy()[once].tolist() == positions[once].tolist()
+    assert dev_table.tolist() == want_table.tolist()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prefill", [[], [(70, 70)], [(30000, 30000), (1, 5), (6000, 6000)]])
+def test_rows_that_no_request_owns_among_many(prefill):
+    """More decode rows than one workgroup looks after, and more rows than are marked at a time; some decodes twice or refused."""
+    n = len(prefill)
+    rng = np.random.default_rng(18)
+    meta, table, free, n_blocks, n_rows = make_tables(prefill, [1 + int(x) for x in rng.integers(0, 40, 20000)], 16, seed=18, pad=9000)
+    # (the decode with the most new blocks keeps them: what is changed has none)
+    for r in np.flatnonzero((meta[:, 2] - 1) % 16 != 0)[:4000].tolist():
+        if r < n:
+            continue
+        meta[r, 0] = int(rng.choice([-1, 20000, meta[r, 0], int(rng.integers(0, 20000))]))
+    for gap in ([0] if n < 2 else [0, 2500]):
+        if gap:
+            meta[n - 1, 0] += gap
+        prm = make_params(n_prefill=n, n_decode=20000, block=16, n_blocks=n_blocks, rows=len(meta), max_blocks=table.shape[1])
+        tables = pod.TokenTables(prm, n_rows)
+        tables.slots.fill_(5)
+        dev_table = torch.from_numpy(table).cuda()
+        tables.build(torch.from_numpy(meta).cuda(), torch.from_numpy(free).cuda(), dev_table)
+        slots, positions, owners, want_table = owned_rows_reference(meta, n, 20000, 16, len(free), free, table, n_rows, len(meta), n_blocks)
+        once = owners <= 1
+        assert (owners == 0).sum() > 9000
+        assert np.array_equal(tables.slots.cpu().numpy()[once], slots[once])
+        assert np.array_equal(tables.positions.cpu().numpy()[once], positions[once])
+        assert np.array_equal(dev_table.cpu().numpy(), want_table)
