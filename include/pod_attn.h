@@ -357,7 +357,9 @@ pod_status pod_attn_forward_static(const void *prefill_q, const void *decode_q,
  * With fewer free blocks than the batch needs nothing is taken: block_table is left as it is, every slot is -1 and report
  * says how many blocks are missing.  A request that cannot be (q_len < 1, kv_len < q_len, a decode with q_len other than
  * 1, cache_row outside the cache, kv_len beyond its row, q_start outside the rows) takes no blocks, and those of its rows
- * that exist and are no other request's get slot -1 and position 0.  A row whose token lies in a block entry outside [0, n_blocks) gets slot -1 as well.
+ * that exist and are no other request's get slot -1 and position 0.  A row whose token lies in a block entry outside
+ * [0, n_blocks) gets slot -1 as well.  Decode rows lie behind as many rows as the prefill requests name, refused ones too:
+ * where report names more than n_rows rows, the decode requests behind the last row take no blocks and are not served.
  * Requests that share a cache_row must not need blocks for it, and a free list must not name a block twice, or one that the
  * cache does not have; of a row that two accepted requests name either may be written.
  */

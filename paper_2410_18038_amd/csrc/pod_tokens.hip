@@ -103,8 +103,25 @@ __global__ __launch_bounds__(kWgThreads) void token_tables(TableArgs a)
     uint32_t any = 0u;
 #pragma unroll
     for (int w = 0; w < kWavesPerWg; ++w) { before += part[w][0]; total += part[w][1]; prows += part[w][2]; refused += part[w][3]; any |= odd[w]; }
-    const bool enough = total <= a.n_free;
     const int64_t covered = prows + a.n_decode;
+    const bool beyond = covered > a.n_rows;
+    if (__builtin_expect(beyond, 0)) {
+        // Decode requests whose rows lie behind the last one take nothing: no row would enter their blocks.
+        int64_t lost = 0, lost_before = 0;
+        for (int r = a.n_prefill + tid; r < n_req; r += kWgThreads) {
+            const Request x = read_request(a, r);
+            if (!x.ok || prows + x.start < a.n_rows) continue;
+            lost += x.fresh;
+            lost_before += r < first_req ? x.fresh : 0;
+        }
+        lost = wave_sum(lost); lost_before = wave_sum(lost_before);
+        __syncthreads();
+        if (lane == 0) { part[wave][0] = lost_before; part[wave][1] = lost; }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWavesPerWg; ++w) { before -= part[w][0]; total -= part[w][1]; }
+    }
+    const bool enough = total <= a.n_free;
     if (b == 0 && tid == 0) {
         a.report[0] = enough ? (int32_t)total : 0;
         a.report[1] = enough ? 0 : (int32_t)min(total - a.n_free, (int64_t)0x7fffffff);
@@ -113,7 +130,6 @@ __global__ __launch_bounds__(kWgThreads) void token_tables(TableArgs a)
     }
     // Row `at` is token `pos` of request x, whose new blocks are free_blocks[taken ..].
     auto write_row = [&](const Request &x, int64_t at, int pos, int64_t taken) {
-        if (at >= a.n_rows) return;
         int slot = -1;
         if (a.block_size == 0) {
             slot = x.row * a.per_row + pos;
@@ -138,6 +154,7 @@ __global__ __launch_bounds__(kWgThreads) void token_tables(TableArgs a)
         const int r = first_req + tid;
         Request x{};
         if (r < n_req) x = read_request(a, r);
+        if (beyond && prows + x.start >= a.n_rows) x = Request{};
         // exclusive prefix sum over the workgroup's requests (a decode takes one block at the most)
         const uint64_t takes = __ballot(x.fresh > 0);
         __syncthreads();

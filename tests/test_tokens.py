@@ -789,3 +789,38 @@ def test_rows_that_no_request_owns_among_many(prefill):
         assert np.array_equal(tables.slots.cpu().numpy()[once], slots[once])
         assert np.array_equal(tables.positions.cpu().numpy()[once], positions[once])
         assert np.array_equal(dev_table.cpu().numpy(), want_table)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,n_rows,changes", [
+    ("two rows short", 95, {}), ("no decode row", 93, {}), ("a refused prompt of many tokens", 105, {(1, 1): 1 << 30}),
+    ("a refused prompt of more than there are rows for", 105, {(1, 1): 28, (1, 2): 27}), ("a row short, the free list as well", 96, {})])
+def test_decodes_behind_the_last_row_take_no_blocks(name, n_rows, changes):
+    """What the report says was taken is what the table's rows have got: a block taken for a row that is not there would be lost."""
+    meta, table, free, n_blocks, _ = make_tables([(40, 50), (20, 20), (33, 90)], [17, 1, 33, 49], 16, seed=19, missing=1 if "free" in name else 0)
+    meta[3:, 0] = [0, 2, 1, 3]
+    for (request, column), value in changes.items():
+        meta[request, column] = value
+    prm = make_params(n_prefill=3, n_decode=4, block=16, n_blocks=n_blocks, rows=len(meta), max_blocks=table.shape[1])
+    tables = pod.TokenTables(prm, n_rows)
+    tables.slots.fill_(5)
+    dev_table = torch.from_numpy(table).cuda()
+    tables.build(torch.from_numpy(meta).cuda(), torch.from_numpy(free).cuda(), dev_table)
+    prows = int(meta[:3, 1].sum())
+    served = [r for r in range(7) if (r != 1 or not changes) and (r < 3 or prows + meta[r, 0] < n_rows)]
+    need = [-(-int(meta[r, 2]) // 16) - -(-int(meta[r, 2] - meta[r, 1]) // 16) for r in served]
+    # ("the free list as well": a block short for the whole batch, exactly enough without the decode left out)
+    assert sum(need) <= len(free) and ("free" not in name or sum(need) == len(free))
+    want = table.copy()
+    taken = 0
+    slots = np.full(n_rows, -1)
+    for r, n in zip(served, need):
+        start, q, kv, row = meta[r].tolist()
+        held = -(-(kv - q) // 16)
+        want[row, held:held + n] = free[taken:taken + n]
+        taken += n
+        at = start + (prows if r >= 3 else 0)
+        slots[at:at + q] = [want[row, t // 16] * 16 + t % 16 for t in range(kv - q, kv)]
+    assert dev_table.tolist() == want.tolist()
+    assert tables.report.tolist() == [taken, 0, 1 if changes else 0, prows + 4]
+    assert tables.slots.tolist() == slots.tolist()
