@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -491,12 +492,14 @@ def _device(device):
     return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
 
 
-_KIND = ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "block_size", "kv_order")
+_KIND = ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "block_size", "kv_order", "n_blocks or n_cache_rows", "kv_seq_stride")
 
 
 def _kind(p: Params):
-    """What the calls of one layer have to have in common, as _KIND names it."""
-    return p.dtype, p.n_q_heads, p.n_kv_heads, p.head_dim, p.block_size, p.kv_order
+    """What the calls of one layer have to have in common, as _KIND names it: the heads, and the cache that a slot names a place
+    of (blocks of a paged one, rows and their length of a contiguous one)."""
+    cache = (p.n_blocks, 0) if p.block_size > 0 else (p.n_cache_rows, p.kv_seq_stride)
+    return (p.dtype, p.n_q_heads, p.n_kv_heads, p.head_dim, p.block_size, p.kv_order) + cache
 
 
 class Rope:
@@ -532,6 +535,7 @@ class TokenTables:
     def __init__(self, params: Params, n_rows: int, *, device="cuda"):
         import torch
         self.params, self.n_rows, self.device, self.kind = params, int(n_rows), _device(device), _kind(params)
+        self.requests = params.n_prefill, params.n_decode
         self.slots = torch.empty(self.n_rows, dtype=torch.int32, device=self.device)
         self.positions = torch.empty(self.n_rows, dtype=torch.int32, device=self.device)
         self.report = torch.zeros(4, dtype=torch.int32, device=self.device)
@@ -670,15 +674,21 @@ class HybridAttention:
               self.ws_ptr, self.ws_bytes, mode, _stream_of(dev))
         return out
 
+    @functools.cached_property
+    def _shape(self):
+        return _kind(self.params), (self.params.n_prefill, self.params.n_decode)
+
     def forward_tokens(self, batch, append: TokenAppend, tables: TokenTables, q, k, v, out=None, mode=MODE_FUSED):
         """One layer of the batch from its projections: the new tokens are put into the cache at ``tables``' slots, then the
         attention reads them.  q, k, v: [rows, heads * head_dim] in the order of the output rows; rows behind the batch are
         padding.  The queries of ``batch`` are not read.  Returns the output rows."""
         n = batch.n_rows
-        kind = _kind(self.params)
+        kind, requests = self._shape
         if append.kind != kind or tables.kind != kind:
             differing = [name for name, *of in zip(_KIND, kind, append.kind, tables.kind) if len(set(of)) > 1]
             raise ValueError(f"{', '.join(differing)} in the plan, {kind}, differ from those of the append, {append.kind}, or the tables, {tables.kind}")
+        if tables.requests != requests:
+            raise ValueError(f"tables for {tables.requests} prefill and decode requests beside a plan for {requests}")
         if q.shape[0] < n:
             raise ValueError(f"{q.shape[0]} rows of projections for a batch of {n}")
         rows = append(q, k, v, tables.slots, tables.positions, batch.k_cache, batch.v_cache)

@@ -824,3 +824,30 @@ def test_decodes_behind_the_last_row_take_no_blocks(name, n_rows, changes):
     assert dev_table.tolist() == want.tolist()
     assert tables.report.tolist() == [taken, 0, 1 if changes else 0, prows + 4]
     assert tables.slots.tolist() == slots.tolist()
+
+
+def test_a_layer_refuses_slots_of_another_cache_and_rows_of_another_batch():
+    """A slot of a contiguous cache is row * length + token: read with another length it is another request's token."""
+    batch = wl.make_batch("other", prefill=[], decode_kv_lens=[5], n_q_heads=8, n_kv_heads=2, head_dim=128, dtype=wl.BF16, seed=1)
+    q = k = v = torch.zeros(1, 8)
+    for mine, others in [(dict(block=0), [dict(max_len=48), dict(max_len=65), dict(rows=9)]), (dict(), [dict(n_blocks=63)])]:
+        for other in others:
+            ours, theirs = make_params(**mine), make_params(**{**mine, **other})
+            attn = pod.HybridAttention.__new__(pod.HybridAttention)
+            attn.params = ours
+            for a, t in [(theirs, ours), (ours, theirs), (theirs, theirs)]:
+                with pytest.raises(ValueError, match="in the plan"):
+                    attn.forward_tokens(batch, pod.TokenAppend(a, device="cpu"), pod.TokenTables(t, 4, device="cpu"), q, k, v)
+    attn = pod.HybridAttention.__new__(pod.HybridAttention)
+    attn.params = make_params(n_prefill=1, n_decode=3)
+    for counts in [(0, 3), (1, 2), (2, 3), (3, 1)]:
+        theirs = make_params(n_prefill=counts[0], n_decode=counts[1])
+        with pytest.raises(ValueError, match="beside a plan for"):
+            attn.forward_tokens(batch, pod.TokenAppend(theirs, device="cpu"), pod.TokenTables(theirs, 4, device="cpu"), q, k, v)
+    # the length of a paged cache's rows and the table's width name no place
+    attn = pod.HybridAttention.__new__(pod.HybridAttention)
+    attn.params = make_params(n_decode=1)
+    theirs = make_params(n_decode=1, rows=3, max_blocks=5)
+    theirs.kv_seq_stride = 640
+    with pytest.raises(ValueError, match="slots must|q must"):
+        attn.forward_tokens(batch, pod.TokenAppend(theirs, device="cpu"), pod.TokenTables(theirs, 1, device="cpu"), q, k, v)
