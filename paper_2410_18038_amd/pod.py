@@ -678,6 +678,10 @@ class HybridAttention:
     def _shape(self):
         return _kind(self.params), (self.params.n_prefill, self.params.n_decode)
 
+    @functools.cached_property
+    def _row_counts(self):
+        return self.info.n_prefill_rows, self.params.n_decode
+
     def forward_tokens(self, batch, append: TokenAppend, tables: TokenTables, q, k, v, out=None, mode=MODE_FUSED):
         """One layer of the batch from its projections: the new tokens are put into the cache at ``tables``' slots, then the
         attention reads them.  q, k, v: [rows, heads * head_dim] in the order of the output rows; rows behind the batch are
@@ -689,6 +693,9 @@ class HybridAttention:
             raise ValueError(f"{', '.join(differing)} in the plan, {kind}, differ from those of the append, {append.kind}, or the tables, {tables.kind}")
         if tables.requests != requests:
             raise ValueError(f"tables for {tables.requests} prefill and decode requests beside a plan for {requests}")
+        rows = batch.n_prefill_rows, batch.n_decode
+        if rows != self._row_counts:
+            raise ValueError(f"a batch of {rows} prefill and decode rows beside a plan for {self._row_counts}")
         if q.shape[0] < n:
             raise ValueError(f"{q.shape[0]} rows of projections for a batch of {n}")
         rows = append(q, k, v, tables.slots, tables.positions, batch.k_cache, batch.v_cache)

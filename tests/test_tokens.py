@@ -846,8 +846,23 @@ def test_a_layer_refuses_slots_of_another_cache_and_rows_of_another_batch():
             attn.forward_tokens(batch, pod.TokenAppend(theirs, device="cpu"), pod.TokenTables(theirs, 4, device="cpu"), q, k, v)
     # the length of a paged cache's rows and the table's width name no place
     attn = pod.HybridAttention.__new__(pod.HybridAttention)
-    attn.params = make_params(n_decode=1)
+    attn.params, attn.info = make_params(n_decode=1), pod.PlanInfo()
     theirs = make_params(n_decode=1, rows=3, max_blocks=5)
     theirs.kv_seq_stride = 640
     with pytest.raises(ValueError, match="slots must|q must"):
         attn.forward_tokens(batch, pod.TokenAppend(theirs, device="cpu"), pod.TokenTables(theirs, 1, device="cpu"), q, k, v)
+
+
+def test_a_layer_refuses_a_batch_of_other_rows_than_the_plan():
+    """The attention writes the plan's rows: those of a batch with fewer would end before it does."""
+    attn = pod.HybridAttention.__new__(pod.HybridAttention)
+    attn.params, attn.info = make_params(n_prefill=1, n_decode=2), pod.PlanInfo(n_prefill_rows=7)
+    append, tables = pod.TokenAppend(attn.params, device="cpu"), pod.TokenTables(attn.params, 40, device="cpu")
+    x = torch.zeros(40, 8)
+    for prefill, decode in [([(6, 6)], [5, 9]), ([(8, 8)], [5, 9]), ([(7, 9)], [5]), ([(7, 9)], [5, 5, 5]), ([], [5, 9])]:
+        batch = wl.make_batch("other", prefill=prefill, decode_kv_lens=decode, n_q_heads=8, n_kv_heads=2, head_dim=128, dtype=wl.BF16, seed=1)
+        with pytest.raises(ValueError, match="rows beside a plan for"):
+            attn.forward_tokens(batch, append, tables, x, x, x)
+    batch = wl.make_batch("mine", prefill=[(7, 9)], decode_kv_lens=[5, 9], n_q_heads=8, n_kv_heads=2, head_dim=128, dtype=wl.BF16, seed=1)
+    with pytest.raises(ValueError, match="q must"):
+        attn.forward_tokens(batch, append, tables, x, x, x)
