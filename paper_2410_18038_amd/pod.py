@@ -267,9 +267,13 @@ def pod_attn_plan_create_scored(params: Params, scores: Optional[Scores], seq_me
         value = getattr(scores, name)
         if value is None:
             continue
-        a = np.ascontiguousarray(value, dtype=dtype)
+        given = np.asarray(value)
+        with np.errstate(invalid="ignore", over="ignore"):
+            a = np.ascontiguousarray(given, dtype=dtype)
         if a.shape != (size,):
             raise ValueError(f"{name} must hold {size} values, not {a.shape}")
+        if dtype == np.int32 and not (a == given).all():                     # (numpy wraps and truncates without a word)
+            raise ValueError(f"{name} holds values that are no 32-bit integers")
         kept.append(a)
         ptr[name] = a.ctypes.data_as(ctypes.POINTER(ctype))
     raw = ScoresParams(scores.logit_cap, scores.window, ptr.get("slopes"), ptr.get("doc_start"), ptr.get("prefix_len"))

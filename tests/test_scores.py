@@ -613,3 +613,18 @@ def test_a_layer_with_a_window_from_its_projections():
     want, tol = reference(seen, scores)
     assert (np.abs(wl.as_f64(out) - want) <= tol).all()
     attn.close()
+
+
+def test_masks_that_are_no_32_bit_integers_are_refused():
+    """An array of 64-bit integers or of floats would be wrapped or cut off on its way to the plan, and mask something else."""
+    b = wl.config_batch(1)
+    plan = lambda **kw: pod.pod_attn_plan_create_scored(plain_params(b), pod.Scores(**kw), b.seq_meta)
+    n_req = len(b.seq_meta)
+    for name, size in (("doc_start", b.n_rows), ("prefix_len", n_req)):
+        for bad in (2.0 ** 32, 2 ** 32 + 5, -2 ** 32, 0.5, float("nan"), float("inf"), 2 ** 31):
+            values = np.zeros(size, np.int64 if isinstance(bad, int) else np.float64)
+            values[-1] = bad
+            with np.errstate(invalid="ignore"), pytest.raises((ValueError, OverflowError)):
+                plan(**{name: values})
+        for good in (np.full(size, 3, np.int64), np.full(size, 3.0), [3] * size, torch.full((size,), 3)):
+            plan(**{name: good}).close()
