@@ -202,6 +202,9 @@ void       pod_attn_plan_destroy(pod_attn_plan *plan);
  * no block (a window's old blocks can be given back).  (Visible values that are infinite
  * make a result infinite or NaN, as their weighted sum does, or NaN where a decode row re-reads them for keys that do not exist.)
  * With POD_MODE_FLAG_NO_COMBINE decode rows that see nothing are not written either.
+ * A score is capped to within 2^-20.7 of itself where the scores beside it (those of up to 32 rows with up to 64 keys, seen or
+ * not) are below half of the cap, and to within 2^-22 of the cap where one is not; the bound of half is a tenth for caps of about
+ * 1e6 times softmax_scale and more, and less for still larger ones.
  */
 typedef struct {
     float   logit_cap;          /* >= 0; 0: scores are not capped.  At most 1e20, and within a factor of 1e20 of

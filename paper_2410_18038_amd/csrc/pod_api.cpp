@@ -147,11 +147,18 @@ pod::CappedArgs make_capped(const pod::Plan &p, const pod::ScoredArgs &a)
     double power = 1.4426950408889634 * p.logit_cap * k;
     s.cap_log2 = p.logit_cap * 1.4426950408889634f;
     s.cap_exp = (float)(2.0 * 1.4426950408889634 * k);
-    for (int i = 0; i < 4; ++i, power *= k * k) s.cap_poly[i] = (float)(power * fit[i]);
-    // Coefficients that leave the range of 32 bits: for caps far above the scores only |y| <= 1/50, where the upper two do
-    // not count; for caps far below them the polynomial is not used.
-    const double last = std::fabs(power / (k * k) * fit[3]);
-    s.cap_limit = (float)((last < 1e-30 ? 0.02 : last > 1e30 ? -1.0 : 0.5) / k);
+    // Coefficients that leave the range of 32 bits: caps far below the scores do not use the polynomial; for caps far above
+    // them it has the terms that 32 bits hold, and an end at which those are still within 2^-20.7 of the score.  (At a softmax_scale of 0.09, scores behind
+    // it are within 2^-23 of the cap: with four terms up to caps of 8e4 and three up to 1e8 that is below 2^-19 of them.)
+    const double ends[5] = {0.0, 0.0005, 0.03, 0.1, 0.5};
+    int terms = 0;
+    double last = 0.0;
+    for (int i = 0; i < 4; ++i, power *= k * k) {
+        last = std::fabs(power * fit[i]);
+        s.cap_poly[i] = terms == i && last >= 1.2e-38 ? (float)(power * fit[i]) : 0.f;
+        if (terms == i && last >= 1.2e-38) ++terms;
+    }
+    s.cap_limit = (float)((last > 1e30 ? -1.0 : ends[terms]) / k);
     return s;
 }
 

@@ -628,3 +628,41 @@ def test_masks_that_are_no_32_bit_integers_are_refused():
                 plan(**{name: values})
         for good in (np.full(size, 3, np.int64), np.full(size, 3.0), [3] * size, torch.full((size,), 3)):
             plan(**{name: good}).close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cap", [2000.0, 6e4, 7e5, 3e6])
+def test_scores_well_below_a_cap_of_thousands_keep_their_digits(cap):
+    """Dot products and their scale are exact here (whole numbers below 2^24 and a power of two), so that what is left of the
+    tolerance is the cap's: 2^-20.7 of a score, doubled for the difference of two, and the softmax weights' and the result's
+    halves of a step.  Each row sees two keys with values 1 and -1 whose scores are 2 to 4 in a hundred of the cap and at most 1 apart."""
+    rng = np.random.default_rng(int(cap))
+    n, d = 256, 128
+    batch = wl.make_batch("pairs", prefill=[(n, n)], decode_kv_lens=[2] * 64, n_q_heads=2, n_kv_heads=2, head_dim=d, dtype=wl.F16, seed=3,
+                          block_size=16, softmax_scale=1.0)
+    scale = 2.0 ** -4
+    batch = dataclasses.replace(batch, softmax_scale=scale, k_cache=torch.zeros_like(batch.k_cache), v_cache=torch.ones_like(batch.v_cache),
+                                prefill_q=torch.zeros_like(batch.prefill_q), decode_q=torch.zeros_like(batch.decode_q))
+    # keys: 1 in the first eight channels; the ninth is 1 for every second key, whose values are -1
+    batch.k_cache[..., :8] = 1.0
+    batch.k_cache[:, 1::2, :, 8] = 1.0
+    batch.v_cache[:, 1::2] = -1.0
+    q = np.zeros((n + 64, 2, d))
+    q[..., :8] = rng.integers(int(0.02 * cap / scale / 8), int(0.04 * cap / scale / 8), (n + 64, 2, 1)).clip(1, 60000)
+    q[..., 8] = rng.integers(-16, 17, (n + 64, 2))
+    q = torch.from_numpy(q).half()
+    batch.prefill_q.copy_(q[:n])
+    batch.decode_q.copy_(q[n:])
+    got = wl.as_f64(run(batch, pod.Scores(logit_cap=cap, window=2))[0])
+    q = wl.as_f64(q)
+    base, step = q[..., :8].sum(-1) * scale, q[..., 8] * scale
+    assert (base <= 2 ** 24 * scale).all()
+    even, odd = cap * np.tanh(base / cap), cap * np.tanh((base + step) / cap)
+    w = 1 / (1 + np.exp(odd - even))                                     # of the key whose value is 1
+    want = 2 * w - 1
+    want[0] = 1.0                                                        # the prompt's first row sees one key
+    delta = 2 * 2.0 ** -20.7 * np.abs(even) + 2.0 ** -23 * np.abs(even)
+    tol = 2.0 ** -11 * 1.01 * (2 + np.abs(want)) + 2 * w * (1 - w) * delta + 2.0 ** -18
+    err = np.abs(got - want[..., None]).max(-1)
+    print("cap", cap, "of the tolerance", float((err / tol).max()), "error", float(err.max()), flush=True)
+    assert (err <= tol).all()
