@@ -150,7 +150,8 @@ typedef struct {
     int32_t prefill_ratio;      /* roles per compute unit, prefill : decode                      */
     int32_t decode_ratio;
     int32_t fused_grid;         /* workgroups of the fused launch (persistent, <= 2 per unit); with
-                                   prefill requests alone the launch has n_prefill_items instead  */
+                                   prefill requests alone the launch has n_prefill_items instead, and plans
+                                   with changed scores may have a workgroup per item (see there)  */
     int32_t n_compute_units;
     int64_t n_prefill_rows;     /* sum of q_len over prefill requests                            */
     int64_t n_partial_rows;     /* rows of fp32 partial output held in the workspace             */
@@ -217,7 +218,9 @@ typedef struct {
 
 /* pod_attn_plan_create for such scores (NULL: plain causal ones, the same plan as without).  The plan keeps what it needs of
  * the arrays, and works with every entry point and mode but POD_MODE_FLAG_PREFILL_HEAVY (POD_ERR_UNSUPPORTED).  Work that no
- * row sees is not planned: a window makes the work of a decode request that of its window. */
+ * row sees is not planned: a window makes the work of a decode request that of its window.  Where a plain plan would choose the
+ * prefill-heavy configuration, POD_MODE_FUSED of such a plan launches a workgroup for every prefill item and four decode
+ * units, as with POD_MODE_FLAG_CTA_PARALLEL, and the persistent workgroups only with a trace or an event log; both give the same bits. */
 pod_status pod_attn_plan_create_scored(const pod_attn_params *params, const pod_attn_scores *scores,
                                        const int32_t *seq_meta_host, pod_attn_plan **plan);
 pod_status pod_attn_plan_info_get(const pod_attn_plan *plan, pod_attn_plan_info *info);

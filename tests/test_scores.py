@@ -666,3 +666,63 @@ def test_scores_well_below_a_cap_of_thousands_keep_their_digits(cap):
     err = np.abs(got - want[..., None]).max(-1)
     print("cap", cap, "of the tolerance", float((err / tol).max()), "error", float(err.max()), flush=True)
     assert (err <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block", [16, 0])
+@pytest.mark.parametrize("name", ["cap", "cap and slopes", "slopes"])
+def test_plans_of_heavy_prompts_launch_a_workgroup_per_item(name, block):
+    """512 items and more, as long as the decode stream: the launch that POD_MODE_FUSED takes by itself there, which kernel it
+    is, rows of it against the definition, and the bits of the other launches (persistent ones with a trace or an event log)."""
+    from torch.profiler import ProfilerActivity, profile
+    n_kv, heads, kv_heads, d = 16384, 32, 4, 128
+    batch = wl.make_batch("heavy", prefill=[(2048, n_kv)], decode_kv_lens=[n_kv - 5 * i for i in range(16)], n_q_heads=heads, n_kv_heads=kv_heads,
+                          head_dim=d, dtype=wl.BF16, seed=51, block_size=block, device="cuda:0")
+    scores = pod.Scores(logit_cap=20.0 if "cap" in name else 0.0, slopes=slopes(heads) if "slopes" in name else None)
+    attn = pod.HybridAttention(batch, scores=scores)
+    assert attn.info.n_prefill_items >= 2 * attn.info.n_compute_units and attn.info.fused_grid <= 2 * attn.info.n_compute_units
+    torch.cuda.synchronize()
+
+    def kernels(call):
+        with profile(activities=[ProfilerActivity.CUDA]) as prof:
+            result = call()
+            torch.cuda.synchronize()
+        return {k for e in prof.key_averages() for k in ("fused_cta_scored", "fused_scored", "prefill_scored", "decode_scored") if "pod::" + k in e.key}, result
+
+    taken, out = kernels(lambda: attn.forward(batch))
+    assert taken == {"fused_cta_scored"}
+    for mode in ("serial", "streams", "fused_cta", "fused"):
+        assert torch.equal(attn.forward(batch, mode=pod.MODES[mode]), out), mode
+    for on, off in ((attn.enable_trace, attn.disable_trace), (attn.enable_event_log, attn.disable_event_log)):
+        on()
+        taken, again = kernels(lambda: attn.forward(batch))
+        off()
+        assert taken == {"fused_scored"} and torch.equal(again, out)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        again = attn.forward(batch)
+    side.synchronize()
+    assert torch.equal(again, out)
+    for r, row, q in ((0, 0, batch.prefill_q[0]), (0, 777, batch.prefill_q[777]), (0, 2047, batch.prefill_q[2047]), (1, 2048, batch.decode_q[0]),
+                      (16, 2063, batch.decode_q[15])):
+        n = n_kv - 2048 + row + 1 if r == 0 else int(batch.seq_meta[r, 2])
+        cache_row = int(batch.seq_meta[r, 3])
+        for h in (0, 9, 31):
+            kvh = h * kv_heads // heads
+            if block:
+                blocks = batch.block_table[cache_row, :-(-n // block)].long()
+                k, v = (c[blocks, :, kvh].reshape(-1, d)[:n].double().cpu().numpy() for c in (batch.k_cache, batch.v_cache))
+            else:
+                k, v = (c[cache_row, :n, kvh].double().cpu().numpy() for c in (batch.k_cache, batch.v_cache))
+            s = k @ q[h].double().cpu().numpy() * batch.softmax_scale
+            if scores.logit_cap:
+                s = scores.logit_cap * np.tanh(s / scores.logit_cap)
+            if scores.slopes is not None:
+                s = s - scores.slopes[h] * np.arange(n - 1, -1, -1)
+            w = np.exp(s - s.max())
+            w /= w.sum()
+            size = w @ np.abs(v)
+            err = np.abs(out[row, h].double().cpu().numpy() - w @ v)
+            # half a step of the weights in the sum and in what it is divided by and of the result; scores in 32 bits
+            assert (err <= 2.0 ** -8 * 1.01 * (2 * size + np.abs(w @ v)) + size * 2.0 ** -12).all(), (row, h)
+    attn.close()
