@@ -211,7 +211,8 @@ typedef struct {
     float   logit_cap;          /* >= 0; 0: scores are not capped.  At most 1e20, and within a factor of 1e20 of
                                    softmax_scale                                                  */
     int32_t window;             /* >= 0; 0: no window                                             */
-    const float   *slopes;      /* host [n_q_heads], finite, or NULL; |slope| <= 1e20 min(1, softmax_scale) */
+    const float   *slopes;      /* host [n_q_heads], finite, or NULL; |slope| <= 1e20 min(1, softmax_scale),
+                                   and softmax_scale >= 1e-30                                     */
     const int32_t *doc_start;   /* host [rows of out], >= 0, or NULL                              */
     const int32_t *prefix_len;  /* host [n_prefill + n_decode], >= 0, or NULL                     */
 } pod_attn_scores;

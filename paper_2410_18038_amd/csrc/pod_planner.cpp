@@ -123,6 +123,8 @@ pod_status read_scores(const pod_attn_scores &scores, const pod_attn_params &prm
     plan.scored = true;
     plan.logit_cap = scores.logit_cap;
     if (scores.slopes) {
+        // (the kernels add slope / softmax_scale to dot products)
+        if (prm.softmax_scale < 1e-30f) { err = "softmax_scale is too small for slopes"; return POD_ERR_INVALID_ARG; }
         plan.slopes.assign((size_t)prm.n_q_heads + kMaxGroup, 0.f);
         for (int h = 0; h < prm.n_q_heads; ++h) {
             if (!std::isfinite(scores.slopes[h])) { err = fmt("slope of head %lld is not finite", h); return POD_ERR_INVALID_ARG; }

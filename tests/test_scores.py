@@ -726,3 +726,17 @@ def test_plans_of_heavy_prompts_launch_a_workgroup_per_item(name, block):
             # half a step of the weights in the sum and in what it is divided by and of the result; scores in 32 bits
             assert (err <= 2.0 ** -8 * 1.01 * (2 * size + np.abs(w @ v)) + size * 2.0 ** -12).all(), (row, h)
     attn.close()
+
+
+def test_slopes_beside_a_scale_that_has_no_reciprocal_are_refused():
+    """1 / softmax_scale is infinite for a subnormal scale, and times a slope of 0 no number."""
+    b = wl.config_batch(1)
+    for scale, refused in ((1e-40, True), (1e-38, True), (9e-31, True), (2e-30, False), (1.0, False)):
+        params = plain_params(b, softmax_scale=scale)
+        pod.pod_attn_plan_create_scored(params, pod.Scores(window=5), b.seq_meta).close()
+        if refused:
+            with pytest.raises(pod.PodError, match="too small for slopes") as e:
+                pod.pod_attn_plan_create_scored(params, pod.Scores(slopes=[0.0] * b.n_q_heads), b.seq_meta)
+            assert e.value.status == -1
+        else:
+            pod.pod_attn_plan_create_scored(params, pod.Scores(slopes=[0.0] * b.n_q_heads), b.seq_meta).close()
