@@ -24,8 +24,8 @@ __device__ __forceinline__ int divide(int t, int divisor, uint32_t magic, int &r
 // Tables.  One launch and nothing shared between workgroups: each one adds up the blocks of all requests before its own
 // (exclusive prefix sum: request r takes free_blocks[before_r ..]) and of the whole batch (does the list hold enough?)
 // from the request lengths themselves, 16 bytes a request that every workgroup finds in its L2, and then writes its own
-// rows.  What bounds it is the launch and two dependent round trips (256 decodes 3.4 us, 6 prompts and 500 decodes, 27K rows,
-// 4.7).  A decode request is a thread; the tokens of a prefill request are dealt to several workgroups.
+// rows.  What bounds it is the launch and two dependent round trips (256 decodes 3.6 us, 6 prompts and 500 decodes, 27K rows,
+// 4.3, a launch in a graph of 200).  A decode request is a thread; the tokens of a prefill request are dealt to several workgroups.
 // Rows without an owner are none where requests begin one behind the other and none is refused, which each thread sees from its
 // requests; only other batches are gone through again, 2048 rows a workgroup, their owners marked in LDS (decodes in another
 // order: 3.6 -> 4.5 and 4.3 -> 5.3 us; prompts in another order, 27K rows, 4.3 -> 9.0).
@@ -209,7 +209,7 @@ hipError_t launch_tables(const TableArgs &a, hipStream_t stream)
 // pair's turns per position as a fraction of 2^64 times the position, whose upper word is the angle as a signed fraction
 // of a turn to 2^-32, for every position; the sine unit takes turns.
 // What bounds it is memory for many rows (8192 rows, 32 / 8 heads of 128 channels, 201 MB: 42 us, 4.8 TB/s, from memory and 33
-// again and again; 8192 x 32 / 32 heads, 403 MB: 79 us, 5.1 TB/s) and the launch for few (16 rows 3.0 us).
+// again and again; 8192 x 32 / 32 heads, 403 MB: 79 us, 5.1 TB/s) and the launch for few (16 rows 2.7 us in a graph of 200).
 // 54 and 11.8 us with one wavefront a row, angles worked out by every lane and the loads behind the slot's.
 // ------------------------------------------------------------------------------------------
 template <int DT> struct Elem;
