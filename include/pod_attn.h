@@ -367,6 +367,8 @@ pod_status pod_attn_forward_static(const void *prefill_q, const void *decode_q,
  * that exist and are no other request's get slot -1 and position 0.  A row whose token lies in a block entry outside
  * [0, n_blocks) gets slot -1 as well.  Decode rows lie behind as many rows as the prefill requests name, refused ones too:
  * where report names more than n_rows rows, the decode requests behind the last row take no blocks and are not served.
+ * A batch that report says is not served whole must not go on to the attention, which reads block_table as it is: entries of
+ * the blocks that were not taken name none.
  * Requests that share a cache_row must not need blocks for it, and a free list must not name a block twice, or one that the
  * cache does not have; of a row that two accepted requests name either may be written.
  */

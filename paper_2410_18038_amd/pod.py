@@ -534,7 +534,9 @@ class TokenTables:
     """Slots and positions of the new tokens of batches of one shape, and the blocks they take.
 
     ``build`` may be called once per step and recorded into a graph; it fills ``slots`` and ``positions`` (int32 [n_rows],
-    rows behind the batch are padding) and ``report`` (blocks taken, blocks missing, requests refused, rows)."""
+    rows behind the batch are padding) and ``report`` (blocks taken, blocks missing, requests refused, rows).  A batch of which
+    blocks are missing, requests refused or rows more than ``n_rows`` must not go on to the attention: its block table lacks
+    blocks."""
 
     def __init__(self, params: Params, n_rows: int, *, device="cuda"):
         import torch
